@@ -300,6 +300,107 @@ hc_status hc_restore_context_mixed(hc_ctx* ctx, const hc_store* hidden_store,
                                    const int32_t* d_block_table, int32_t n_blocks,
                                    void* compute_stream, void* copy_stream);
 
+/* ---- KV cache in 4 bits -------------------------------------------------------------------
+ * A layer may have, beside its bf16 pool or in its place, a pool of pages in 4 bits: 17 / 64 of the bytes.  32
+ * neighbouring channels of a token's K or V row share a scale, the smallest power of two s with max|x| <= 7 s (2^-125 to
+ * 2^125), and every value is stored as the nearest of +-s * {0, 0.5, 1, 1.5, 2, 3, 4, 6}, ties to the even code: at most
+ * half a step from it.  What is read back is exact in bf16.  A group that holds an infinity or a NaN becomes NaN.
+ *   pool: uint8 [num_pages][n_kv_heads][block_size / 16][17 * head_dim]; the bytes of 16 tokens of a head are
+ *     K codes  8 * head_dim  [token][channel / 2]                                  (even channel: low four bits)
+ *     V codes  8 * head_dim  [token / 4][slice of 16][token % 4][head_dim / 32]    (slice r: channels r * head_dim / 16 ..)
+ *     K scales head_dim / 2  [token][channel / 32]                                 (biased exponents; 255: NaN)
+ *     V scales head_dim / 2  [token / 4][channel / 32][token % 4]
+ * Needs head_dim 64, 128 or 256 and block_size >= 16 (HC_EINVAL).  Block tables are as for bf16 pages; whether both pools of a
+ * layer go by the same table is the caller's choice.  The calls of this section and of the next launch on the context's device,
+ * whichever is current, and allocate nothing; they may be captured. */
+
+/* Bytes of one page of a 4-bit pool: n_kv_heads * block_size / 16 * 17 * head_dim. */
+hc_status hc_kv4_page_bytes(const hc_model_desc* desc, int64_t* out_bytes);
+
+/* Register one layer's 4-bit pool (borrowed; 16-byte aligned; num_pages as in hc_set_kv_pool). */
+hc_status hc_set_kv4_pool(hc_ctx* ctx, int32_t layer, void* d_pool, int64_t num_pages);
+
+/* Token rows into the 4-bit pages of a ragged batch of contexts (a prompt's K and V, or one new token of each context):
+ *   d_rows         bf16  [h_total_tokens][K row | V row], 2 * d_kv wide, K rotated, as of hc_gather_kv
+ *   d_positions    int32 [h_total_tokens]     positions within the row's context; those of one context must differ
+ *   d_cu_seqlens   int32 [n_seq + 1]          context s owns rows cu[s] .. cu[s + 1] - 1, cu[0] = 0; NULL with n_seq = 1: all rows
+ *                                             are one context's
+ *   d_block_tables int32 [n_seq][max_blocks]
+ * Other slots of the pages stay as they are.  Rows with an invalid position or page, and rows of no context, are skipped
+ * and flagged as in hc_restore_kv. */
+hc_status hc_quantize_kv(hc_ctx* ctx, int32_t layer, const void* d_rows, const int32_t* d_positions,
+                         int32_t h_total_tokens, const int32_t* d_cu_seqlens, int32_t n_seq,
+                         const int32_t* d_block_tables, int32_t max_blocks, void* stream);
+/* The same for tokens of one context that stand in the layer's bf16 pages (as a restore has put them): read through
+ * d_block_table, written through d_block_table4. */
+hc_status hc_quantize_kv_pages(hc_ctx* ctx, int32_t layer, const int32_t* d_positions, int32_t n_tok,
+                               const int32_t* d_block_table, int32_t n_blocks, const int32_t* d_block_table4,
+                               int32_t n_blocks4, void* stream);
+/* Rows back out of 4-bit pages, in bf16 (exact): d_rows is written, skipped rows are left as they were. */
+hc_status hc_dequantize_kv(hc_ctx* ctx, int32_t layer, void* d_rows, const int32_t* d_positions,
+                           int32_t h_total_tokens, const int32_t* d_cu_seqlens, int32_t n_seq,
+                           const int32_t* d_block_tables, int32_t max_blocks, void* stream);
+
+/* Attention of queries over the 4-bit cache of their contexts, one layer: a decoding step, a few tokens a context, or
+ * prompts on histories, ragged.
+ *   d_q            bf16  [h_total_q][n_q_heads][head_dim], rotated; q_stride elements from one token to the next
+ *   d_positions    int32 [h_total_q]     a query at position p sees keys at positions max(0, p - window + 1) .. min(p, keys - 1) of its
+ *                                        context; window 0: from 0 on.  Positions may stand in any order and need not be those
+ *                                        of stored tokens; p = 2^31 - 1 sees all keys, p < 0 none.
+ *   d_cu_q         int32 [n_seq + 1]     context s owns queries cu[s] .. cu[s + 1] - 1, cu[0] = 0
+ *   d_kv_lens      int32 [n_seq]         keys of the context (those of this step's queries included, when they are stored)
+ *   d_block_tables int32 [n_seq][max_blocks]
+ *   scale          > 0: weights are softmax(scale * q . k)
+ *   d_out          bf16  [h_total_q][n_q_heads][head_dim], out_stride elements from one token to the next
+ *   d_lse          fp32  [h_total_q][n_q_heads], or NULL: log of the sum of exp(scale * q . k) (natural), for joining with attention over
+ *                        other keys
+ * A query that sees no key gets zeros, and -infinity in d_lse.  Queries of no context (from cu[n_seq] on) are left as they
+ * were.  Keys on pages that are none of the pool's count as unseen and raise HC_DEV_BAD_PAGE; key counts below 0 or beyond
+ * the table are clamped and raise HC_DEV_BAD_POSITION.  What unseen slots hold does not matter.
+ * h_max_q and h_max_kv should be the most queries and keys of a context: the launch is laid out by them, results do not
+ * depend on them but for the order of sums.
+ *   d_workspace    16-byte aligned, workspace_bytes >= hc_attend_kv4_workspace of the same sizes (HC_EINVAL); used by this launch
+ *                  alone until it is done: calls that may run at the same time, and graphs that may, need one each.  NULL when the
+ *                  size is 0.
+ * q_stride and out_stride: multiples of 8, at least n_q_heads * head_dim.  At most 65535 contexts (HC_ERANGE). */
+hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_stride, const int32_t* d_positions,
+                        int32_t h_total_q, const int32_t* d_cu_q, const int32_t* d_kv_lens, int32_t n_seq, int32_t h_max_q,
+                        int32_t h_max_kv, const int32_t* d_block_tables, int32_t max_blocks, float scale, int32_t window,
+                        void* d_out, int64_t out_stride, float* d_lse, void* d_workspace, int64_t workspace_bytes,
+                        void* stream);
+/* Bytes of workspace of such a call (0 where it needs none); host only. */
+hc_status hc_attend_kv4_workspace(const hc_model_desc* desc, int32_t n_seq, int32_t h_total_q, int32_t h_max_q,
+                                  int32_t h_max_kv, int64_t* out_bytes);
+
+/* ---- pages as a whole ------------------------------------------------------------------------
+ * Block tables are int32 [n_rows][max_blocks] on the device, shared by all layers; `pools` names the pools that go by
+ * them: HC_POOL_KV (bf16), HC_POOL_KV4 (4 bits) or both.  Every layer needs each of them (HC_ESTATE), all of the same
+ * number of pages (HC_EINVAL). */
+enum { HC_POOL_KV = 1, HC_POOL_KV4 = 2 };
+
+/* Fork contexts: row h_to_rows[i] of the tables becomes a context of the first h_n_tok[i] tokens of row h_from_rows[i].  Full blocks
+ * are shared (the pages of both tables are the same); where h_n_tok[i] ends inside a block, the page h_new_pages[i] (a
+ * free one of the caller's; not read otherwise) takes its place in the new row, and the tokens in use are copied to it in every
+ * layer (of a 4-bit page: the 16-token blocks in use).  The rest of the row becomes -1.
+ * The four arrays are HOST arrays of n_fork entries, read during the call only.  Rows in range, h_n_tok[i] within the table, new
+ * pages within the pools (HC_ERANGE); no row is the target of two forks or both source and target, no page is given
+ * twice (HC_EINVAL).  A fork whose source has no valid page to copy, or the new page itself there, gets -1 for that
+ * block and raises HC_DEV_BAD_PAGE. */
+hc_status hc_fork_pages(hc_ctx* ctx, int32_t pools, int32_t* d_block_tables, int32_t n_rows, int32_t max_blocks,
+                        const int32_t* h_from_rows, const int32_t* h_to_rows, const int32_t* h_n_tok,
+                        const int32_t* h_new_pages, int32_t n_fork, void* stream);
+
+/* Compact a cache: pages that no entry of the tables names are freed, the others become pages 0 .. live - 1 of the pools.
+ * Of the live pages those below `live` stay; the others move, the lowest to the lowest free place, the next to the
+ * next, in every layer, and the tables follow:
+ *   d_tables_in, d_tables_out  int32 [n_rows][max_blocks], may be the same array; entries < 0 become -1, entries beyond the
+ *                              pools too, and raise HC_DEV_BAD_PAGE; pages may be named any number of times
+ *   d_plan  int32 [2 + 2 * num_pages], written: pages live, pages moved, the new number of every page (-1: freed), then
+ *                              (from, to) of every move; what is behind the last move is left as it was
+ * All tables of contexts that are to live have to be in the call.  At most 2^20 pages (HC_ERANGE). */
+hc_status hc_compact_pages(hc_ctx* ctx, int32_t pools, const int32_t* d_tables_in, int32_t* d_tables_out, int32_t n_rows,
+                           int32_t max_blocks, int32_t* d_plan, void* stream);
+
 /* ---- two-stage saving of new hidden states (Section 4.2.2; Section 5 "Pipelined state
  * transmission", "Storage management") -------------------------------------------------
  * Stage 1: the inputs of one layer for the whole running batch (rows of several contexts

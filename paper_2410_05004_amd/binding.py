@@ -9,6 +9,7 @@ _LIB_FILE = os.environ.get("HCACHE_LIB") or os.path.join(HERE, "libhcache.so")
 HC_OK, HC_EINVAL, HC_ERANGE, HC_EALIGN, HC_ENOMEM, HC_EHIP, HC_ESTATE = 0, -1, -2, -3, -4, -5, -6
 HC_DEV_BAD_POSITION, HC_DEV_BAD_PAGE = 1, 2
 HC_NORM_RMS, HC_NORM_LAYER = 0, 1
+HC_POOL_KV, HC_POOL_KV4 = 1, 2
 _STATUS_NAMES = {0: "HC_OK", -1: "HC_EINVAL", -2: "HC_ERANGE", -3: "HC_EALIGN", -4: "HC_ENOMEM",
                  -5: "HC_EHIP", -6: "HC_ESTATE"}
 
@@ -75,6 +76,16 @@ def _load():
         "hc_poison_staging": (i32, [vp, vp]),
         "hc_gather_kv": (i32, [vp, i32, vp, vp, i32, vp, i32, vp]),
         "hc_scatter_kv": (i32, [vp, i32, vp, vp, i32, vp, i32, vp]),
+        "hc_kv4_page_bytes": (i32, [p(ModelDesc), p(i64)]),
+        "hc_set_kv4_pool": (i32, [vp, i32, vp, i64]),
+        "hc_quantize_kv": (i32, [vp, i32, vp, vp, i32, vp, i32, vp, i32, vp]),
+        "hc_quantize_kv_pages": (i32, [vp, i32, vp, i32, vp, i32, vp, i32, vp]),
+        "hc_dequantize_kv": (i32, [vp, i32, vp, vp, i32, vp, i32, vp, i32, vp]),
+        "hc_attend_kv4": (i32, [vp, i32, vp, i64, vp, i32, vp, vp, i32, i32, i32, vp, i32, C.c_float, i32,
+                                vp, i64, vp, vp, i64, vp]),
+        "hc_attend_kv4_workspace": (i32, [p(ModelDesc), i32, i32, i32, i32, p(i64)]),
+        "hc_fork_pages": (i32, [vp, i32, vp, i32, i32, vp, vp, vp, vp, i32, vp]),
+        "hc_compact_pages": (i32, [vp, i32, vp, vp, i32, i32, vp, vp]),
         "hc_restore_contexts": (i32, [vp, vp, i32, vp, vp, vp, i32, vp, vp]),
         "hc_restore_context_mixed": (i32, [vp, vp, vp, i32, i64, i32, i32, i32, vp, i32, vp, vp]),
         "hc_set_loader": (i32, [vp, i32]),
@@ -112,7 +123,9 @@ EXPORTED = ("hc_last_error hc_version hc_validate_desc hc_create hc_destroy hc_s
             "hc_saver_flush hc_partition_layers hc_gather_kv hc_scatter_kv "
             "hc_restore_context_mixed hc_set_layer_weights_affine hc_saver_save_layer_deferred "
             "hc_saver_fence hc_restore_kv_layers hc_restore_contexts hc_timing_end_stats "
-            "hc_restore_context_static hc_static_stage_bytes hc_poison_staging hc_diag_mfma_duty hc_diag_tile_map hc_set_split hc_diag_split_plan hc_diag_route hc_diag_tile").split()
+            "hc_restore_context_static hc_static_stage_bytes hc_poison_staging hc_diag_mfma_duty hc_diag_tile_map hc_set_split hc_diag_split_plan hc_diag_route hc_diag_tile "
+            "hc_kv4_page_bytes hc_set_kv4_pool hc_quantize_kv hc_quantize_kv_pages hc_dequantize_kv hc_attend_kv4 "
+            "hc_attend_kv4_workspace hc_fork_pages hc_compact_pages").split()
 
 
 def _check(status):
@@ -184,6 +197,19 @@ def partition_layers(n_layers, io_h, io_kv, c_h, c_token):
     _check(lib.hc_partition_layers(n_layers, io_h, io_kv, c_h, c_token, C.byref(lh), C.byref(lo),
                                    C.byref(comp)))
     return lh.value, lo.value, comp.value
+
+
+def kv4_page_bytes(desc):
+    out = C.c_int64(0)
+    _check(lib.hc_kv4_page_bytes(C.byref(desc), C.byref(out)))
+    return out.value
+
+
+def attend_kv4_workspace(desc, n_seq, total_q, max_q, max_kv):
+    """Bytes of workspace that Context.attend_kv4 needs for these sizes."""
+    out = C.c_int64(0)
+    _check(lib.hc_attend_kv4_workspace(C.byref(desc), n_seq, total_q, max_q, max_kv, C.byref(out)))
+    return out.value
 
 
 def _ptr(x):
@@ -287,6 +313,39 @@ class Context:
     def scatter_kv(self, layer, d_rows, d_positions, n_tok, d_block_table, n_blocks, stream=0):
         _check(lib.hc_scatter_kv(self._h, layer, _ptr(d_rows), _ptr(d_positions), n_tok,
                                  _ptr(d_block_table), n_blocks, stream))
+
+    def set_kv4_pool(self, layer, d_pool, num_pages):
+        _check(lib.hc_set_kv4_pool(self._h, layer, _ptr(d_pool), num_pages))
+
+    def quantize_kv(self, layer, d_rows, d_positions, total_tokens, d_cu_seqlens, n_seq, d_block_tables, max_blocks, stream=0):
+        _check(lib.hc_quantize_kv(self._h, layer, _ptr(d_rows), _ptr(d_positions), total_tokens, _ptr(d_cu_seqlens), n_seq,
+                                  _ptr(d_block_tables), max_blocks, stream))
+
+    def quantize_kv_pages(self, layer, d_positions, n_tok, d_block_table, n_blocks, d_block_table4, n_blocks4, stream=0):
+        _check(lib.hc_quantize_kv_pages(self._h, layer, _ptr(d_positions), n_tok, _ptr(d_block_table), n_blocks,
+                                        _ptr(d_block_table4), n_blocks4, stream))
+
+    def dequantize_kv(self, layer, d_rows, d_positions, total_tokens, d_cu_seqlens, n_seq, d_block_tables, max_blocks, stream=0):
+        _check(lib.hc_dequantize_kv(self._h, layer, _ptr(d_rows), _ptr(d_positions), total_tokens, _ptr(d_cu_seqlens), n_seq,
+                                    _ptr(d_block_tables), max_blocks, stream))
+
+    def attend_kv4(self, layer, d_q, q_stride, d_positions, total_q, d_cu_q, d_kv_lens, n_seq, max_q, max_kv, d_block_tables,
+                   max_blocks, scale, window, d_out, out_stride, d_lse, d_workspace, workspace_bytes, stream=0):
+        _check(lib.hc_attend_kv4(self._h, layer, _ptr(d_q), q_stride, _ptr(d_positions), total_q, _ptr(d_cu_q), _ptr(d_kv_lens),
+                                 n_seq, max_q, max_kv, _ptr(d_block_tables), max_blocks, scale, window, _ptr(d_out), out_stride,
+                                 _ptr(d_lse), _ptr(d_workspace), workspace_bytes, stream))
+
+    def fork_pages(self, pools, d_block_tables, n_rows, max_blocks, from_rows, to_rows, n_tok, new_pages, stream=0):
+        """The last four are host sequences, one entry a fork."""
+        import numpy as np
+        lists = [np.ascontiguousarray(v, dtype=np.int32) for v in (from_rows, to_rows, n_tok, new_pages)]
+        assert all(v.ndim == 1 and v.shape == lists[0].shape for v in lists)
+        _check(lib.hc_fork_pages(self._h, pools, _ptr(d_block_tables), n_rows, max_blocks, *[_ptr(v) for v in lists],
+                                 len(lists[0]), stream))
+
+    def compact_pages(self, pools, d_tables_in, d_tables_out, n_rows, max_blocks, d_plan, stream=0):
+        _check(lib.hc_compact_pages(self._h, pools, _ptr(d_tables_in), _ptr(d_tables_out), n_rows, max_blocks, _ptr(d_plan),
+                                    stream))
 
     def set_loader(self, mode):
         _check(lib.hc_set_loader(self._h, mode))

@@ -22,10 +22,9 @@ hc_status fail_hip(hipError_t e, const char* what) {
 }
 void clear_error() { g_last_error.clear(); }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
-static hc_status check_desc(const hc_model_desc* d) {
+hc_status check_desc(const hc_model_desc* d) {
   if (!d) return fail(HC_EINVAL, "desc is null");
   if (d->n_layers <= 0) return fail(HC_EINVAL, "n_layers must be positive");
   if (d->d_model <= 0 || d->d_model % 64 != 0)
@@ -49,7 +48,7 @@ static hc_status check_desc(const hc_model_desc* d) {
   return HC_OK;
 }
 
-static hc_status check_layer(const hc_ctx* ctx, int32_t layer) {
+hc_status check_layer(const hc_ctx* ctx, int32_t layer) {
   if (!ctx) return fail(HC_EINVAL, "ctx is null");
   if (layer < 0 || layer >= ctx->desc.n_layers) return fail(HC_ERANGE, "layer out of range");
   return HC_OK;

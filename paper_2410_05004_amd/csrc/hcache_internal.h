@@ -707,6 +707,10 @@ void clear_error();
 
 struct hc_ctx;
 namespace hc {
+// Argument checks shared by the entry points.
+hc_status check_desc(const hc_model_desc* d);
+hc_status check_layer(const hc_ctx* ctx, int32_t layer);
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 // Validated launch of the fused kernel for one layer (shared by every restore entry point).
 // positions == nullptr means position = pos_base + row.
 hc_status restore_layer(hc_ctx* ctx, int32_t layer, const void* d_hidden,
@@ -731,6 +735,8 @@ struct hc_layer_state {
   float2* affine = nullptr;      // owned; present when the layer has a shift or a bias, or LayerNorm
   uint16_t* pool = nullptr;      // borrowed
   int64_t num_pages = 0;
+  uint8_t* pool4 = nullptr;      // borrowed: the layer's 4-bit pool
+  int64_t num_pages4 = 0;
 };
 
 struct hc_ctx {
