@@ -310,7 +310,7 @@ hc_status hc_restore_context_mixed(hc_ctx* ctx, const hc_store* hidden_store,
  *     V codes  8 * head_dim  [token / 4][slice of 16][token % 4][head_dim / 32]    (slice r: channels r * head_dim / 16 ..)
  *     K scales head_dim / 2  [token][channel / 32]                                 (biased exponents; 255: NaN)
  *     V scales head_dim / 2  [token / 4][channel / 32][token % 4]
- * Needs head_dim 64, 128 or 256 and block_size >= 16 (HC_EINVAL).  Block tables are as for bf16 pages; whether both pools of a
+ * Needs head_dim 64, 128 or 256, block_size >= 16 and pages below 2 GiB (HC_EINVAL).  Block tables are as for bf16 pages; whether both pools of a
  * layer go by the same table is the caller's choice.  The calls of this section and of the next launch on the context's device,
  * whichever is current, and allocate nothing; they may be captured. */
 
@@ -355,8 +355,8 @@ hc_status hc_dequantize_kv(hc_ctx* ctx, int32_t layer, void* d_rows, const int32
  *   d_lse          fp32  [h_total_q][n_q_heads], or NULL: log of the sum of exp(scale * q . k) (natural), for joining with attention over
  *                        other keys
  * A query that sees no key gets zeros, and -infinity in d_lse.  Queries of no context (from cu[n_seq] on) are left as they
- * were.  Keys on pages that are none of the pool's count as unseen and raise HC_DEV_BAD_PAGE; key counts below 0 or beyond
- * the table are clamped and raise HC_DEV_BAD_POSITION.  What unseen slots hold does not matter.
+ * were.  Keys on pages that are none of the pool's count as unseen and raise HC_DEV_BAD_PAGE; key counts below 0, beyond
+ * the table or beyond 2^30 are clamped and raise HC_DEV_BAD_POSITION.  What unseen slots hold does not matter.
  * h_max_q and h_max_kv should be the most queries and keys of a context: the launch is laid out by them, results do not
  * depend on them but for the order of sums.
  *   d_workspace    16-byte aligned, workspace_bytes >= hc_attend_kv4_workspace of the same sizes (HC_EINVAL); used by this launch

@@ -216,11 +216,10 @@ def _ptr(x):
     """Address of a torch tensor / numpy array / int (None -> NULL)."""
     if x is None:
         return None
-    if isinstance(x, int):
-        return x
-    if hasattr(x, "data_ptr"):
+    try:                                     # the common case first: this is most of what a call costs on the host
         return x.data_ptr()
-    return x.ctypes.data
+    except AttributeError:
+        return x if isinstance(x, int) else x.ctypes.data
 
 
 class Context:

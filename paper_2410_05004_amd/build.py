@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhcache.so")
 SOURCES = ["api.cpp", "store.cpp", "saver.cpp", "restore_mode0.hip", "restore_mode1.hip",
            "restore_mode2.hip", "aux_kernels.hip", "static_restore.hip", "cache_api.cpp", "kv4_rows.hip",
-           "kv4_attend.hip", "pages.hip"]
+           "kv4_attend.hip", "kv4_prompt.hip", "pages.hip"]
 
 
 def hipcc_path():

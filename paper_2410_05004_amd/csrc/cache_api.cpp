@@ -32,14 +32,15 @@ class OnDevice {
   bool moved_ = false;
 };
 
+int64_t kv4_page_bytes(const hc_model_desc& d) {
+  return (int64_t)d.n_kv_heads * (d.block_size / kSubTokens) * sub_bytes(d.head_dim);
+}
+
 hc_status check_kv4(const hc_model_desc& d) {
   if (!attend_head_dim(d.head_dim)) return fail(HC_EINVAL, "the 4-bit cache needs head_dim 64, 128 or 256");
   if (d.block_size < kSubTokens) return fail(HC_EINVAL, "the 4-bit cache needs block_size >= 16");
+  if (kv4_page_bytes(d) > INT_MAX) return fail(HC_EINVAL, "a page of the 4-bit cache must stay below 2 GiB");   // kernels hold it in 32 bits
   return HC_OK;
-}
-
-int64_t kv4_page_bytes(const hc_model_desc& d) {
-  return (int64_t)d.n_kv_heads * (d.block_size / kSubTokens) * sub_bytes(d.head_dim);
 }
 
 hc_status check_layer4(const hc_ctx* ctx, int32_t layer) {
@@ -339,7 +340,7 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
   a.scale_log2 = scale * 1.44269504089f;
   a.row_tiles = plan.row_tiles;
   a.n_split = plan.n_split;
-  HC_HIP(launch_attend(a, d.head_dim, static_cast<hipStream_t>(stream)));
+  HC_HIP(launch_attend(a, d.head_dim, plan.row_blocks, static_cast<hipStream_t>(stream)));
   return HC_OK;
 }
 

@@ -42,6 +42,7 @@ enum class Kv4Move { kRowsToCodes, kPagesToCodes, kCodesToRows };
 hipError_t launch_kv4_rows(const Kv4RowsArgs& a, Kv4Move move, hipStream_t stream);
 
 // Attention over the 4-bit pool.
+constexpr int64_t kMaxKeys = 1 << 30;       // of a context: keys and what is added to them stay within 32 bits
 struct AttendArgs {
   const uint16_t* q;
   int64_t q_stride, out_stride;            // elements from one token to the next
@@ -62,11 +63,14 @@ struct AttendArgs {
   int32_t row_tiles, n_split;
 };
 struct AttendPlan {
-  int32_t row_tiles, n_split;
+  int32_t row_blocks;                      // blocks of 16 rows of a workgroup; kv4_prompt.hip from 8 on
+  int32_t row_tiles, n_split;              // workgroups along a context's rows, shares of the keys
   int64_t workspace;                       // bytes
 };
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv);
 bool attend_head_dim(int head_dim);
-hipError_t launch_attend(const AttendArgs& a, int head_dim, hipStream_t stream);
+int attend_rows_blocks(int head_dim);      // row blocks of a workgroup of launch_attend_rows
+hipError_t launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_attend(const AttendArgs& a, int head_dim, int row_blocks, hipStream_t stream);
 
 }  // namespace hc

@@ -7,276 +7,202 @@
 // sum need no exchange between columns, and W goes from the result registers of the first product into the
 // operand registers of the second as it stands -- key 4 * q4 + v of either half of 32 keys is register v of quarter q4
 // there, and element v (+ 4) of its operand here, an order that V^T's operand has to share and the cache is laid out in.
+// No lane of a wave goes another way than the others while results are in registers: where these are many, the compiler
+// has been seen to put a copy that it needs for all lanes into a branch that some had not taken (sums of the second 16 rows were
+// wrong at 256 channels, the registers in question traced in the generated code).  What concerns some lanes is selected, and what
+// several would store alike they all do.
 // Decoded keys and values are exact in bf16; W is rounded to bf16 (2^-9 relative, without a bias, which averages out over
 // the keys), sums and statistics are fp32.
-#include "kv4.h"
+#include "kv4_device.h"
 
 namespace hc {
 
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-
-constexpr float kNegInf = -__builtin_inff();
-// The running top follows a row's maximum only when that has grown by more than this (of base 2): weights then reach
-// 2^8 instead of 1, which costs nothing in floating point, and most steps rescale nothing.
-constexpr float kTopSlack = 8.f;
-
-__device__ __forceinline__ uint32_t decode2(uint32_t w, float scale, int byte) {
-  switch (byte) {
-    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
-    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
-    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
-    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
-  }
-}
-
-// The conversion reads the exponent field of its scale alone: what else the shifted word holds does no harm
-// (checked for every exponent, with the other bits zero, one and mixed).
-__device__ __forceinline__ float scale_of(uint32_t word, int byte) {
-  return __uint_as_float(byte == 3 ? word >> 1 : word << (23 - 8 * byte));
-}
-
-__device__ __forceinline__ float across_quarters_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float across_quarters_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
-
-// A lane's bytes of 16 keys of a head.
-template <int HD>
-struct Raw {
-  static constexpr int kWords = HD / 32;
-  uint32_t k[kWords], v[kWords];
-  uint32_t ks, vs;
-};
-
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t* to, const uint8_t* from) {
-  if constexpr (N == 2) {
-    const u32x2 x = *reinterpret_cast<const u32x2*>(from);
-    to[0] = x[0]; to[1] = x[1];
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(from + 4 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) to[i + j] = x[j];
-    }
-  }
-}
-
-// `at`: the 16 keys' first byte, the same for the whole wave
-template <int HD>
-__device__ __forceinline__ void load_raw(Raw<HD>& r, const uint8_t* at, int l16, int q4) {
-  load_words<HD / 32>(r.k, at + l16 * (HD / 2) + q4 * (HD / 8));
-  load_words<HD / 32>(r.v, at + v_codes_at(HD) + (q4 * 16 + l16) * (HD / 8));
-  const uint8_t* ks = at + k_scales_at(HD) + l16 * (HD / 32);
-  if constexpr (HD == 64)       r.ks = ks[q4 >> 1];
-  else if constexpr (HD == 128) r.ks = ks[q4];
-  else                          r.ks = *reinterpret_cast<const uint16_t*>(ks + 2 * q4);
-  r.vs = *reinterpret_cast<const uint32_t*>(at + v_scales_at(HD) + (q4 * (HD / 32) + l16 * HD / 512) * 4);
-}
-
-// What the queries of 16 rows see.
-struct Rows {
-  int lo, hi;              // this lane's row: keys lo .. hi, none if hi < lo
-  int begin, end;          // of all rows: keys that any row sees
-  int all_lo, all_hi;      // keys that every row sees
-};
-
-// Steps of 32 keys [step, ...) of one wave, every `stride`-th, for 16 rows.
-template <int HD>
-struct Walk {
-  const AttendArgs& a;
-  const int32_t* table;
-  const uint8_t* pool;           // of the KV head
-  int64_t page_bytes;
-  int keys;                      // of the context
-  int bad = 0;
-
-  // first byte of keys [key, key + 16), and 0 in `ok` where the page is none of the pool's
-  __device__ __forceinline__ const uint8_t* place(int key, bool& ok) {
-    const int block = key >> a.block_shift;
-    int page = block < a.max_blocks ? table[block] : 0;
-    ok = page >= 0 && page < a.num_pages;
-    if (!ok) page = 0;
-    return pool + page * page_bytes + ((key & ((1 << a.block_shift) - 1)) >> 4) * sub_bytes(HD);
-  }
-};
-
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) { const int o = __shfl_xor(x, m); x = x < o ? x : o; }
-  return x;
-}
-__device__ __forceinline__ int wave_max(int x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) { const int o = __shfl_xor(x, m); x = x > o ? x : o; }
-  return x;
-}
-
-// Rows of a context and KV head: row r is query r / group, query head r % group of the KV head's.  A workgroup takes 16
-// rows and a share of the keys, its four waves every fourth step of 32 keys.
-template <int HD>
-__global__ __launch_bounds__(256) void attend_few_kernel(const AttendArgs a) {
+// Rows of a context and KV head: row r is query r / group, query head r % group of the KV head's.  A workgroup takes
+// NB blocks of 16 rows and a share of the keys; its four waves take every fourth step of 32 keys, for all the rows.
+// The next step's bytes are fetched into the registers as soon as this step's are decoded: keys before the softmax, values
+// behind the second product.
+template <int HD, int NB>
+__global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) void attend_kernel(const AttendArgs a) {
   constexpr int kSteps = HD / 32;         // matrix ops along the channels
   constexpr int kSlices = HD / 16;        // blocks of 16 channels of the result
   __shared__ float s_out[3][kSlices * 4][64];
-  __shared__ float s_top[4][16], s_sum[4][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q4 = lane >> 4;
+  __shared__ float s_top[4][NB][16], s_sum[4][NB][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q4 = lane >> 4;
   const int split = blockIdx.x % a.n_split, kvh = blockIdx.x / a.n_split, seq = blockIdx.z;
-  int q0 = a.cu_q[seq], q1 = a.cu_q[seq + 1];
+  int q0 = uniform(a.cu_q)[seq], q1 = uniform(a.cu_q)[seq + 1];
   q0 = q0 < 0 ? 0 : q0;
   q1 = q1 > a.total_q ? a.total_q : q1;
-  const int64_t most = (int64_t)a.max_blocks << a.block_shift;
-  int keys = a.kv_lens[seq];
+  const int64_t room = (int64_t)a.max_blocks << a.block_shift, most = room < kMaxKeys ? room : kMaxKeys;
+  int keys = uniform(a.kv_lens)[seq];
   if (keys > most || keys < 0) {
     if (threadIdx.x == 0) atomicOr(a.err, HC_DEV_BAD_POSITION);
     keys = keys < 0 ? 0 : (int)most;
   }
-  const int n_rows = (q1 - q0) * a.group;
-  const int32_t* table = a.block_tables + (size_t)seq * a.max_blocks;
-  const int subs = 1 << (a.block_shift - 4);
-  const int64_t head_bytes = (int64_t)subs * sub_bytes(HD);
-  Walk<HD> walk{a, table, a.pool + kvh * head_bytes, head_bytes * a.n_kv, keys};
+  const int n_rows = (q1 - q0) * a.group, n_tiles = (n_rows + NB * 16 - 1) / (NB * 16);
+  Places places(a, seq, kvh, sub_bytes(HD));
+  bool bad_page = false;
 
-  for (int tile = blockIdx.y; tile * 16 < n_rows; tile += gridDim.y) {
+  // the last rows first: they see the most keys
+  for (int turn = blockIdx.y; turn < n_tiles; turn += gridDim.y) {
+    const int tile = n_tiles - 1 - turn;
+    // ---- this workgroup's share of the keys, in steps of 32: of all that there are, or, if there is a window, of those that any row
+    // sees.  Without one nothing waits for the positions: the table's entries and the rows are on their way together.
+    auto query_of = [&](int nb) __attribute__((always_inline)) {
+      const int r = (tile * NB + nb) * 16 + l16;
+      return (r < n_rows ? r : n_rows - 1) / a.group;
+    };
+    auto head_of = [&](int nb, int query) __attribute__((always_inline)) {
+      const int r = (tile * NB + nb) * 16 + l16;
+      return kvh * a.group + (r < n_rows ? r : n_rows - 1) - query * a.group;
+    };
+    const int lane_key = (lane >> 1) * 128 + (lane & 1) * 16;        // run i of a round: half i % 2 of this wave's step i / 2
+    int first = 0, n_step = (keys + 31) >> 5, share = 0, step = 0, stop = 0;
+    auto take_share = [&]() __attribute__((always_inline)) {
+      share = (n_step + a.n_split - 1) / a.n_split;
+      step = first + split * share;
+      stop = min_of(step + share, first + n_step);
+      step += wave;
+      if (step < stop) places.look_up(step * 32 + lane_key);
+    };
+    if (a.window == 0) take_share();
     // ---- the rows
-    const int r = tile * 16 + l16;
-    const bool row_in = r < n_rows;
-    const int rr = row_in ? r : n_rows - 1;
-    const int qi = rr / a.group, head = kvh * a.group + rr - qi * a.group;
-    const int64_t tok = q0 + qi;
-    const int pos = a.positions[tok];
-    Rows rows;
-    rows.hi = pos < keys - 1 ? pos : keys - 1;
-    rows.lo = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
-    const bool sees = rows.hi >= rows.lo;
-    rows.begin = wave_min(sees ? rows.lo : 0x7fffffff);
-    rows.end = wave_max(sees ? rows.hi + 1 : 0);
-    rows.all_lo = wave_max(rows.lo);
-    rows.all_hi = wave_min(rows.hi);
-    bf16x8 q[kSteps];
-    {
-      const uint16_t* from = a.q + tok * a.q_stride + head * HD + q4 * (HD / 4);
+    int lo[NB], hi[NB];                              // keys that this lane's rows see: none if hi < lo
+    int begin = 0x7fffffff, end = 0, all_lo = 0, all_hi = 0x7fffffff;   // keys that any row sees, and that every row sees
+    bf16x8 q[NB][kSteps];
 #pragma unroll
-      for (int j = 0; j < kSteps; ++j) q[j] = *reinterpret_cast<const bf16x8*>(from + 8 * j);
+    for (int nb = 0; nb < NB; ++nb) {
+      const int qi = query_of(nb), pos = a.positions[q0 + qi];
+      const uint16_t* from = a.q + (q0 + qi) * a.q_stride + head_of(nb, qi) * HD + q4 * (HD / 4);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) q[nb][j] = *reinterpret_cast<const bf16x8*>(from + 8 * j);
+      hi[nb] = pos < keys - 1 ? pos : keys - 1;
+      lo[nb] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+      const bool sees = hi[nb] >= lo[nb];
+      begin = min_of(begin, sees ? lo[nb] : 0x7fffffff);
+      end = max_of(end, sees ? hi[nb] + 1 : 0);
+      all_lo = max_of(all_lo, lo[nb]);
+      all_hi = min_of(all_hi, hi[nb]);
     }
-    // ---- this workgroup's share of the keys, in steps of 32
-    const int first = rows.begin < rows.end ? rows.begin >> 5 : 0;
-    const int n_step = rows.begin < rows.end ? ((rows.end + 31) >> 5) - first : 0;
-    const int share = (n_step + a.n_split - 1) / a.n_split;
-    int step = first + split * share;
-    int stop = step + share;
-    if (stop > first + n_step) stop = first + n_step;
-    step += wave;
-
-    f32x4 o[kSlices];
-#pragma unroll
-    for (int b = 0; b < kSlices; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float top = kNegInf, top_used = 0.f, sum = 0.f;     // top_used: 0 while there is no finite top, so that exp2 of -inf stays 0
-
-    Raw<HD> raw[2], next[2];
-    bool ok[2], next_ok[2];
-    if (step < stop) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) load_raw<HD>(raw[h], walk.place(step * 32 + 16 * h, ok[h]), l16, q4);
+    begin = __builtin_amdgcn_readfirstlane(across_16(begin, min_of));
+    end = __builtin_amdgcn_readfirstlane(across_16(end, max_of));
+    all_lo = __builtin_amdgcn_readfirstlane(across_16(all_lo, max_of));
+    all_hi = __builtin_amdgcn_readfirstlane(across_16(all_hi, min_of));
+    if (a.window != 0) {
+      first = begin < end ? begin >> 5 : 0;
+      n_step = begin < end ? ((end + 31) >> 5) - first : 0;
+      take_share();
     }
-    for (; step < stop; step += 4) {
-      if (step + 4 < stop) {
+
+    f32x4 o[NB][kSlices];
+    float top[NB], used[NB], sum[NB];                // used: the top, 0 while there is no finite one, so that exp2 of -inf stays 0
 #pragma unroll
-        for (int h = 0; h < 2; ++h) load_raw<HD>(next[h], walk.place((step + 4) * 32 + 16 * h, next_ok[h]), l16, q4);
+    for (int nb = 0; nb < NB; ++nb) {
+      top[nb] = kNegInf;
+      used[nb] = sum[nb] = 0.f;
+#pragma unroll
+      for (int b = 0; b < kSlices; ++b) o[nb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    RawK<HD> rk[2];
+    RawV<HD> rv[2];
+    int at = 0, gone = 0, next_gone = 0;             // run of the next fetch; halves without a page, of this step and the next
+    auto next_runs = [&](int s) __attribute__((always_inline)) {       // places of step s
+      if (at == 0) {
+        places.settle(s * 32 + lane_key);
+        places.look_up((s + 128) * 32 + lane_key);
       }
-      const int key0 = step * 32;
-      // ---- S^T = K Q^T
-      f32x4 s[2];
+      next_gone = ~(int)(places.there >> at) & 3;
+    };
+    if (step < stop) {
+      next_runs(step);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        rk[h].load(places.of(h), l16, q4);
+        rv[h].load(places.of(h), l16, q4);
+      }
+      at = 2;
+    }
+    for (; step < stop; step += 4) {
+      const int key0 = step * 32;
+      gone = next_gone;
+      next_runs(step + 4);                           // behind the last step: some page's, not used
+      const uint8_t* next_at[2] = {places.of(at), places.of(at + 1)};
+      at = (at + 2) & 63;
+      // ---- S^T = K Q^T
+      f32x4 s[NB][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[nb][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-          const float ks = scale_of(raw[h].ks, HD == 256 ? j >> 2 : 0);
+          const float ks = scale_of(rk[h].scales, HD == 256 ? j >> 2 : 0);
           u32x4 k;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) k[i] = decode2(raw[h].k[j], ks, i);
-          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), q[j], s[h], 0, 0, 0);
+          for (int i = 0; i < 4; ++i) k[i] = decode2(rk[h].w[j], ks, i);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            s[nb][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), q[nb][j], s[nb][h], 0, 0, 0);
+          }
         }
+        rk[h].load(next_at[h], l16, q4);
       }
       // ---- masks, where a row's first or last key lies in these 32 or a page is missing
-      if (key0 < rows.all_lo || key0 + 31 > rows.all_hi || !ok[0] || !ok[1]) {
+      if (key0 < all_lo || key0 + 31 > all_hi || gone) {
+        asm volatile("");                            // stays a branch: the compiler would mask every step
         bool nan_value = false;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (!ok[h] && key0 + 16 * h < rows.end && key0 + 16 * h + 15 >= rows.begin) walk.bad = HC_DEV_BAD_PAGE;
+          const bool none = gone >> h & 1;
+          if (none && key0 + 16 * h < end && key0 + 16 * h + 15 >= begin) bad_page = true;
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             const int key = key0 + 16 * h + 4 * q4 + v;
-            if (!ok[h] || key < rows.lo || key > rows.hi) s[h][v] = kNegInf;
-            // V of a key that no row sees is taken as zero, whatever its place holds: weight 0 times NaN would be NaN
-            const bool none = !ok[h] || key < rows.begin || key >= rows.end;
-            const uint32_t byte = raw[h].vs >> (8 * v) & 255u;
-            if (none || byte == kNanScale) {
-              raw[h].vs = (raw[h].vs & ~(255u << (8 * v))) | 127u << (8 * v);
-              if constexpr (HD == 64)       raw[h].v[v >> 1] &= v & 1 ? 0x0000ffffu : 0xffff0000u;
-              else if constexpr (HD == 128) raw[h].v[v] = 0;
-              else                          raw[h].v[2 * v] = raw[h].v[2 * v + 1] = 0;
-              nan_value |= !none;
-            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+              if (none || key < lo[nb] || key > hi[nb]) s[nb][h][v] = kNegInf;
           }
+          nan_value |= only_seen<HD>(rv[h], key0 + 16 * h + 4 * q4, begin, end, none);
         }
-        // NaN among the values of keys that some row sees: taken out above, and given to the rows that see them here
-        if (__any(nan_value)) {
-          for (int h = 0; h < 2; ++h) {
-            bool ok_h;
-            const uint8_t* at = walk.place(key0 + 16 * h, ok_h) + v_scales_at(HD);
-            if (!ok_h) continue;
-            for (int t = 0; t < 16; ++t) {
-              const int key = key0 + 16 * h + t;
-              if (key < rows.lo || key > rows.hi) continue;
-              // this lane's results are channels q4 * HD / 4 ..
+        if (__any(nan_value)) {                      // taken out above, given to the rows that see it here
 #pragma unroll
-              for (int g = 0; g < (HD == 256 ? 2 : 1); ++g) {
-                const int group = HD == 64 ? q4 >> 1 : HD == 128 ? q4 : 2 * q4 + g;
-                if (at[((t >> 2) * (HD / 32) + group) * 4 + (t & 3)] != kNanScale) continue;
+          for (int nb = 0; nb < NB; ++nb) {
+            // this lane's results are channels q4 * HD / 4 ..: one group of 32, or two
+            f32x2 poison;
 #pragma unroll
-                for (int b = 0; b < kSlices; ++b)
+            for (int g = 0; g < 2; ++g) poison[g] = nan_values<HD>(places, key0, 32, lo[nb], hi[nb], HD == 256 ? 2 * q4 + g : q4 * HD / 128);
 #pragma unroll
-                  for (int v = 0; v < 4; ++v)
-                    if (HD != 256 || (v >> 1) == g) o[b][v] = __builtin_nanf("");
-              }
-            }
+            for (int b = 0; b < kSlices; ++b)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) o[nb][b][v] += poison[v >> 1];
           }
         }
       }
       // ---- running top and sum
-      float m = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-      m *= a.scale_log2;
-      if (__any(m > top + kTopSlack)) {
-        const float grown = fmaxf(top, across_quarters_max(m));
-        const float used = grown == kNegInf ? 0.f : grown;
-        const float shrink = __builtin_amdgcn_exp2f(top - used);        // 0 for the first keys
-        top = grown;
-        top_used = used;
-        sum *= shrink;
+      bf16x8 w[NB];
 #pragma unroll
-        for (int b = 0; b < kSlices; ++b) o[b] *= shrink;
-      }
-      bf16x8 w;
+      for (int nb = 0; nb < NB; ++nb) {
+        const f32x4 x = s[nb][0], y = s[nb][1];
+        float m = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+        m *= a.scale_log2;
+        if (__any(m > top[nb] + kTopSlack)) {
+          const float grown = fmaxf(top[nb], across_quarters(m, [](float p, float r) { return fmaxf(p, r); }));
+          used[nb] = grown == kNegInf ? 0.f : grown;
+          const float shrink = __builtin_amdgcn_exp2f(top[nb] - used[nb]);        // 0 for the first keys
+          top[nb] = grown;
+          sum[nb] *= shrink;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][v], a.scale_log2, -top_used));
-          sum += e;
-          w[4 * h + v] = (__bf16)e;
+          for (int b = 0; b < kSlices; ++b) o[nb][b] *= shrink;
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][h][v], a.scale_log2, -used[nb]));
+            sum[nb] += e;
+            w[nb][4 * h + v] = (__bf16)e;
+          }
+      }
       // ---- O^T += V^T W^T: byte i of a key's word holds slices 2 i and 2 i + 1
 #pragma unroll
       for (int i = 0; i < HD / 32; ++i) {
@@ -287,151 +213,186 @@ __global__ __launch_bounds__(256) void attend_few_kernel(const AttendArgs a) {
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             const int byte = t * (HD / 32) + i;
-            c[t] = decode2(raw[h].v[byte >> 2], scale_of(raw[h].vs, t), byte & 3);
+            c[t] = decode2(rv[h].w[byte >> 2], scale_of(rv[h].scales, t), byte & 3);
           }
           even[2 * h] = __builtin_amdgcn_perm(c[1], c[0], 0x05040100);
           even[2 * h + 1] = __builtin_amdgcn_perm(c[3], c[2], 0x05040100);
           odd[2 * h] = __builtin_amdgcn_perm(c[1], c[0], 0x07060302);
           odd[2 * h + 1] = __builtin_amdgcn_perm(c[3], c[2], 0x07060302);
         }
-        o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), w, o[2 * i], 0, 0, 0);
-        o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), w, o[2 * i + 1], 0, 0, 0);
-      }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) { raw[h] = next[h]; ok[h] = next_ok[h]; }
-    }
-    if (walk.bad && lane == 0) atomicOr(a.err, walk.bad);
-
-    // ---- the four waves' shares, added up in the waves' order
-    sum = across_quarters_sum(sum);
-    if (q4 == 0) { s_top[wave][l16] = top; s_sum[wave][l16] = sum; }
-    __syncthreads();
-    float best = kNegInf;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) best = fmaxf(best, s_top[i][l16]);
-    const float best_used = best == kNegInf ? 0.f : best;
-    const float mine = __builtin_amdgcn_exp2f(top - best_used);
-    float total = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) total += s_sum[i][l16] * __builtin_amdgcn_exp2f(s_top[i][l16] - best_used);
-    if (wave > 0) {
-#pragma unroll
-      for (int b = 0; b < kSlices; ++b)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) s_out[wave - 1][b * 4 + v][lane] = o[b][v] * mine;
-    }
-    __syncthreads();
-    if (wave == 0 && row_in) {
-      const int64_t row = tok * a.n_q + head;
-      // register (b, v) is channel (4 * q4 + v) * HD / 16 + b
-      if (a.n_split == 1) {
-        const float norm = total == 0.f ? 0.f : 1.f / total;         // a row that sees no key: zeros
-        uint16_t* to = a.out + tok * a.out_stride + head * HD + q4 * (HD / 4);
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int b = 0; b < kSlices; b += 4) {
-            float x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x[i] = (((o[b + i][v] * mine + s_out[0][(b + i) * 4 + v][lane]) + s_out[1][(b + i) * 4 + v][lane]) + s_out[2][(b + i) * 4 + v][lane]) * norm;
-            u32x2 y;
-            y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[0], x[1]}, bf16x2));
-            y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2], x[3]}, bf16x2));
-            *reinterpret_cast<u32x2*>(to + v * kSlices + b) = y;
-          }
-        if (a.lse && q4 == 0) a.lse[row] = best_used * 0.69314718056f + __logf(total);
-      } else {
-        const int64_t n_row = (int64_t)a.total_q * a.n_q;
-        float* to = a.part + (split * n_row + row) * HD + q4 * (HD / 4);
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int b = 0; b < kSlices; b += 4) {
-            f32x4 x;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x[i] = ((o[b + i][v] * mine + s_out[0][(b + i) * 4 + v][lane]) + s_out[1][(b + i) * 4 + v][lane]) + s_out[2][(b + i) * 4 + v][lane];
-            *reinterpret_cast<f32x4*>(to + v * kSlices + b) = x;
-          }
-        if (q4 == 0) {
-          float* ml = a.part + a.n_split * n_row * HD + (split * n_row + row) * 2;
-          ml[0] = best;
-          ml[1] = total;
+        for (int nb = 0; nb < NB; ++nb) {
+          o[nb][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), w[nb], o[nb][2 * i], 0, 0, 0);
+          o[nb][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), w[nb], o[nb][2 * i + 1], 0, 0, 0);
         }
       }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) rv[h].load(next_at[h], l16, q4);
+    }
+
+    // ---- the four waves' shares, added up in the waves' order; a block's results are one wave's to write
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      sum[nb] = across_quarters(sum[nb], [](float p, float r) { return p + r; });
+      s_top[wave][nb][l16] = top[nb];                // from all four quarters
+      s_sum[wave][nb][l16] = sum[nb];
     }
     __syncthreads();
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int writer = nb & 3;
+      float best = kNegInf;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) best = fmaxf(best, s_top[i][nb][l16]);
+      const float best_used = best == kNegInf ? 0.f : best;
+      const float mine = __builtin_amdgcn_exp2f(top[nb] - best_used);
+#pragma unroll
+      for (int b = 0; b < kSlices; ++b) o[nb][b] *= mine;
+      if (wave != writer) {
+        const int at = wave - (wave > writer ? 1 : 0);
+#pragma unroll
+        for (int b = 0; b < kSlices; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s_out[at][b * 4 + v][lane] = o[nb][b][v];
+      }
+      __syncthreads();
+      if (wave == writer && (tile * NB + nb) * 16 < n_rows) {       // places behind the last row have computed that row too and store the same
+        float total = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) total += s_sum[i][nb][l16] * __builtin_amdgcn_exp2f(s_top[i][nb][l16] - best_used);
+        const int qi = query_of(nb), head = head_of(nb, qi);
+        const int64_t tok = q0 + qi, row = tok * a.n_q + head;
+        // register (b, v) is channel (4 * q4 + v) * HD / 16 + b
+        auto joined = [&](int b, int v) __attribute__((always_inline)) {
+          return ((s_out[0][b * 4 + v][lane] + s_out[1][b * 4 + v][lane]) + s_out[2][b * 4 + v][lane]) + o[nb][b][v];
+        };
+        if (a.n_split == 1) {
+          const float norm = total == 0.f ? 0.f : 1.f / total;         // a row that sees no key: zeros
+          uint16_t* to = a.out + tok * a.out_stride + head * HD + q4 * (HD / 4);
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int b = 0; b < kSlices; b += 4) {
+              u32x2 y;
+              y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{joined(b, v) * norm, joined(b + 1, v) * norm}, bf16x2));
+              y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{joined(b + 2, v) * norm, joined(b + 3, v) * norm}, bf16x2));
+              *reinterpret_cast<u32x2*>(to + v * kSlices + b) = y;
+            }
+          if (a.lse) a.lse[row] = best_used * 0.69314718056f + __logf(total);
+        } else {
+          const int64_t n_row = (int64_t)a.total_q * a.n_q;
+          float* to = a.part + (split * n_row + row) * HD + q4 * (HD / 4);
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int b = 0; b < kSlices; b += 4)
+              *reinterpret_cast<f32x4*>(to + v * kSlices + b) = f32x4{joined(b, v), joined(b + 1, v), joined(b + 2, v), joined(b + 3, v)};
+          *reinterpret_cast<f32x2*>(a.part + a.n_split * n_row * HD + (split * n_row + row) * 2) = f32x2{best, total};
+        }
+      }
+      __syncthreads();
+    }
   }
+  if (bad_page && lane == 0) atomicOr(a.err, HC_DEV_BAD_PAGE);
 }
 
-// Joins the shares of a row, in their order: a wave a row.
-template <int HD>
+// Joins the shares of a row, in an order that depends on the sizes alone.  16 lanes read a share, HD / 16 channels each; PARTS such
+// groups go over a row's shares, every PARTS-th, and 16 / PARTS rows are a workgroup's.
+template <int HD, int PARTS>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
-  const int lane = threadIdx.x & 63;
+  constexpr int kPer = HD / 16, kRows = 16 / PARTS;
+  __shared__ float s_x[16][HD + 4], s_total[16];
+  const int group = threadIdx.x >> 4, part = group % PARTS, l16 = threadIdx.x & 15;
   const int64_t n_row = (int64_t)a.total_q * a.n_q;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= n_row) return;
-  const int64_t tok = row / a.n_q;
-  const int head = (int)(row - tok * a.n_q);
-  if (tok < a.cu_q[0] || tok >= a.cu_q[a.n_seq]) return;    // no context's
-  const float* ml = a.part + a.n_split * n_row * HD + row * 2;
+  int64_t row = (int64_t)blockIdx.x * kRows + group / PARTS;
+  const bool in = row < n_row;
+  row = in ? row : n_row - 1;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part + a.n_split * n_row * HD) + row;
   float best = kNegInf;
-  for (int i = lane; i < a.n_split; i += 64) best = fmaxf(best, ml[i * n_row * 2]);
+  for (int i = l16; i < a.n_split; i += 16) best = fmaxf(best, ml[i * n_row][0]);
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) best = fmaxf(best, __shfl_xor(best, m));
+  for (int m = 1; m < 16; m <<= 1) best = fmaxf(best, __shfl_xor(best, m));
   const float used = best == kNegInf ? 0.f : best;
   float total = 0.f;
-  constexpr int kPer = HD / 64;
-  float x[kPer];
+  f32x4 x[kPer / 4];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) x[i] = 0.f;
-  for (int i = 0; i < a.n_split; ++i) {
-    const float w = __builtin_amdgcn_exp2f(ml[i * n_row * 2] - used);
-    total += w * ml[i * n_row * 2 + 1];
-    const float* from = a.part + (i * n_row + row) * HD + lane * kPer;
+  for (int e = 0; e < kPer / 4; ++e) x[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+  for (int i = part; i < a.n_split; i += PARTS) {
+    const f32x2 t = ml[i * n_row];
+    const float w = __builtin_amdgcn_exp2f(t[0] - used);
+    total += w * t[1];
+    const f32x4* from = reinterpret_cast<const f32x4*>(a.part + (i * n_row + row) * HD + l16 * kPer);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] += w * from[e];
+    for (int e = 0; e < kPer / 4; ++e) x[e] += w * from[e];
   }
-  const float norm = total == 0.f ? 0.f : 1.f / total;
-  uint16_t* to = a.out + tok * a.out_stride + head * HD + lane * kPer;
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) to[e] = __builtin_bit_cast(uint16_t, (__bf16)(x[e] * norm));
+  for (int e = 0; e < kPer / 4; ++e) *reinterpret_cast<f32x4*>(&s_x[group][l16 * kPer + 4 * e]) = x[e];
+  if (l16 == 0) s_total[group] = total;
+  __syncthreads();
+  // the row's lanes take its channels
+  const int first = group / PARTS * PARTS;
+  const int64_t tok = row / a.n_q;
+  const int head = (int)(row - tok * a.n_q);
+  if (!in || tok < uniform(a.cu_q)[0] || tok >= uniform(a.cu_q)[a.n_seq]) return;    // no context's
+  total = 0.f;
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) total += s_total[first + i];
+  const float norm = total == 0.f ? 0.f : 1.f / total;
+  const int lane = threadIdx.x - first * 16;
+  for (int c = lane; c < HD; c += PARTS * 16) {
+    float y = 0.f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) y += s_x[first + i][c];
+    a.out[tok * a.out_stride + head * HD + c] = __builtin_bit_cast(uint16_t, (__bf16)(y * norm));
+  }
   if (a.lse && lane == 0) a.lse[row] = used * 0.69314718056f + __logf(total);
 }
 
 bool attend_head_dim(int head_dim) { return head_dim == 64 || head_dim == 128 || head_dim == 256; }
 
+// Blocks of 16 rows of a workgroup.
+static int row_blocks(int head_dim, int64_t rows) {
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : attend_rows_blocks(head_dim);
+}
+
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv) {
   AttendPlan p;
-  const int group = n_q / n_kv;
-  int64_t tiles = ((int64_t)max_q * group + 15) / 16;
+  const int64_t rows = (int64_t)max_q * (n_q / n_kv);
+  p.row_blocks = row_blocks(head_dim, rows);
+  const int64_t tiles = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);
   p.row_tiles = (int)(tiles < 1 ? 1 : tiles > 65535 ? 65535 : tiles);
   const int64_t base = (int64_t)n_seq * n_kv * p.row_tiles;
-  // keys are split until there are some 4096 workgroups, not below 256 keys to one
-  int64_t split = base > 0 ? 4096 / base : 1, most = ((int64_t)max_kv + 255) / 256;
+  // Keys are split until the chip is full: two workgroups a compute unit for prompts and for a context alone, whose shares are
+  // alike, more where contexts differ, so that none of them is long at the end (64 contexts of 2K to 8K keys: 99 us in 1024
+  // workgroups, 89 in 2048, 91 to 99 in 4096; one of 128K keys: 33 us in 2048, 27 in 512); not below 256 keys to one.
+  const int64_t wanted = p.row_blocks > 2 || n_seq == 1 ? 2 * kChipCUs : 8 * kChipCUs;
+  int64_t split = base > 0 ? wanted / base : 1, most = ((int64_t)max_kv + 255) / 256;
   if (split > most) split = most;
-  if (split > 512) split = 512;
   p.n_split = split < 1 ? 1 : (int)split;
   p.workspace = p.n_split > 1 ? (int64_t)p.n_split * total_q * n_q * (head_dim + 2) * 4 : 0;
   return p;
 }
 
 template <int HD>
-static void launch_hd(const AttendArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(attend_few_kernel<HD>, dim3(a.n_split * a.n_kv, a.row_tiles, a.n_seq), dim3(256), 0, stream, a);
+static void launch_hd(const AttendArgs& a, int row_blocks, hipStream_t stream) {
+  const dim3 grid(a.n_split * a.n_kv, a.row_tiles, a.n_seq);
+  if (row_blocks == 1)      hipLaunchKernelGGL((attend_kernel<HD, 1>), grid, dim3(256), 0, stream, a);
+  else if (row_blocks == 2) hipLaunchKernelGGL((attend_kernel<HD, 2>), grid, dim3(256), 0, stream, a);
+  else                      (void)launch_attend_rows(a, HD, stream);
   if (a.n_split > 1) {
     const int64_t n_row = (int64_t)a.total_q * a.n_q;
-    hipLaunchKernelGGL(attend_join_kernel<HD>, dim3((unsigned)((n_row + 3) / 4)), dim3(256), 0, stream, a);
+    if (a.n_split <= 4) hipLaunchKernelGGL((attend_join_kernel<HD, 4>), dim3((unsigned)((n_row + 3) / 4)), dim3(256), 0, stream, a);
+    else                hipLaunchKernelGGL((attend_join_kernel<HD, 16>), dim3((unsigned)n_row), dim3(256), 0, stream, a);
   }
 }
 
-hipError_t launch_attend(const AttendArgs& a, int head_dim, hipStream_t stream) {
+hipError_t launch_attend(const AttendArgs& a, int head_dim, int row_blocks, hipStream_t stream) {
   if (a.total_q <= 0 || a.n_seq <= 0) return hipSuccess;
   switch (head_dim) {
-    case 64: launch_hd<64>(a, stream); break;
-    case 128: launch_hd<128>(a, stream); break;
-    case 256: launch_hd<256>(a, stream); break;
+    case 64: launch_hd<64>(a, row_blocks, stream); break;
+    case 128: launch_hd<128>(a, row_blocks, stream); break;
+    case 256: launch_hd<256>(a, row_blocks, stream); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
