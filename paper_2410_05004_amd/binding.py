@@ -337,10 +337,11 @@ class Context:
     def fork_pages(self, pools, d_block_tables, n_rows, max_blocks, from_rows, to_rows, n_tok, new_pages, stream=0):
         """The last four are host sequences, one entry a fork."""
         import numpy as np
-        lists = [np.ascontiguousarray(v, dtype=np.int32) for v in (from_rows, to_rows, n_tok, new_pages)]
-        assert all(v.ndim == 1 and v.shape == lists[0].shape for v in lists)
-        _check(lib.hc_fork_pages(self._h, pools, _ptr(d_block_tables), n_rows, max_blocks, *[_ptr(v) for v in lists],
-                                 len(lists[0]), stream))
+        lists = np.array((from_rows, to_rows, n_tok, new_pages), dtype=np.int32)       # one array, one address
+        assert lists.ndim == 2
+        at, step = lists.ctypes.data, lists.strides[0]
+        _check(lib.hc_fork_pages(self._h, pools, _ptr(d_block_tables), n_rows, max_blocks, at, at + step, at + 2 * step,
+                                 at + 3 * step, lists.shape[1], stream))
 
     def compact_pages(self, pools, d_tables_in, d_tables_out, n_rows, max_blocks, d_plan, stream=0):
         _check(lib.hc_compact_pages(self._h, pools, _ptr(d_tables_in), _ptr(d_tables_out), n_rows, max_blocks, _ptr(d_plan),

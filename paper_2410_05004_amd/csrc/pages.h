@@ -6,6 +6,7 @@
 namespace hc {
 
 constexpr int kForksPerLaunch = 64;
+constexpr int kForkPiece = 5 * 256;       // 16-byte words of a page that a workgroup copies
 constexpr int kPoolsPerLaunch = 128;      // pools (a layer's bf16 or 4-bit one) per launch
 constexpr int kMaxCompactPages = 1 << 20; // one bit each in a compute unit's LDS
 
@@ -26,7 +27,8 @@ struct ForkArgs {
   int32_t* tables;
   int32_t* err;
   int64_t num_pages;
-  int32_t n_fork, max_blocks, block_shift, with_tables, pieces;
+  int32_t n_fork, max_blocks, block_shift, with_tables;
+  int32_t pieces, shares;                 // of a page (kForkPiece words); of the pools
 };
 hipError_t launch_fork(const ForkArgs& a, hipStream_t stream);
 

@@ -6,12 +6,14 @@ namespace hc {
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 // ---- fork -----------------------------------------------------------------------------------
-// blockIdx: (piece of a page, fork, pool); one more "pool" writes the children's table rows.
+// blockIdx: (piece of a page, fork, share of the pools); the share behind the last writes the children's table rows.
 // A child's row is its parent's for the full blocks, its own page for a part-filled last one, -1 behind it; of that
 // page the tokens in use are copied.  Parents' rows and children's are different rows, so no order matters.
-// Bound: latency for a few forks (table entry, then page), memory for many.
+// Bound: latency for a few forks (the parent's table entry, then the page), memory for many.  A workgroup looks the page up
+// once and copies the same piece of it, up to 20 KiB, in every so-many-th pool.
+constexpr int kForkWords = kForkPiece / 256;   // of a thread
 __global__ __launch_bounds__(256) void fork_kernel(const ForkArgs a) {
-  const int f = blockIdx.y, pool = blockIdx.z;
+  const int f = blockIdx.y, share = blockIdx.z;
   const int n_tok = a.n_tok[f], whole = n_tok >> a.block_shift, rest = n_tok & ((1 << a.block_shift) - 1);
   const int32_t* parent = a.tables + (size_t)a.from[f] * a.max_blocks;
   // the page to copy: valid, and not the one that it is to be copied into
@@ -21,7 +23,7 @@ __global__ __launch_bounds__(256) void fork_kernel(const ForkArgs a) {
     last = parent[whole];
     ok = last >= 0 && last < a.num_pages && last != a.page[f];
   }
-  if (pool == a.pools.n_pools) {
+  if (share == a.shares) {
     if (blockIdx.x) return;
     int32_t* child = a.tables + (size_t)a.to[f] * a.max_blocks;
     for (int b = threadIdx.x; b < a.max_blocks; b += 256)
@@ -30,28 +32,35 @@ __global__ __launch_bounds__(256) void fork_kernel(const ForkArgs a) {
     return;
   }
   if (!rest || !ok) return;
-  const PageShape& s = a.pools.shape[pool >= a.pools.first4];
-  const int run = ((rest + (1 << s.unit_shift) - 1) >> s.unit_shift) * s.unit, total = s.runs * run;
-  u32x4* base = static_cast<u32x4*>(a.pools.pool[pool]);
-  const u32x4* from = base + (size_t)last * s.words;
-  u32x4* to = base + (size_t)a.page[f] * s.words;
-  for (int i0 = blockIdx.x * 1024 + threadIdx.x; i0 < total; i0 += gridDim.x * 1024) {
-    u32x4 v[4];
-    int at[4];
+  for (int kind = 0; kind < 2; ++kind) {
+    const int begin = kind ? a.pools.first4 : 0, end = kind ? a.pools.n_pools : a.pools.first4;
+    if (begin + share >= end) continue;
+    const PageShape& s = a.pools.shape[kind];
+    const int run = ((rest + (1 << s.unit_shift) - 1) >> s.unit_shift) * s.unit, total = s.runs * run;
+    int at[kForkWords];
+    bool in[kForkWords];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * 256;
-      at[u] = i / run * s.stride + i % run;
-      if (i < total) v[u] = from[at[u]];
+    for (int u = 0; u < kForkWords; ++u) {
+      const int i = blockIdx.x * kForkWords * 256 + u * 256 + threadIdx.x;
+      in[u] = i < total;
+      at[u] = run == s.stride ? i : i / run * s.stride + i % run;
     }
+    const size_t from = (size_t)last * s.words, to = (size_t)a.page[f] * s.words;
+    for (int pool = begin + share; pool < end; pool += a.shares) {
+      u32x4* base = static_cast<u32x4*>(a.pools.pool[pool]);
+      u32x4 v[kForkWords];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i0 + u * 256 < total) to[at[u]] = v[u];
+      for (int u = 0; u < kForkWords; ++u)
+        if (in[u]) v[u] = __builtin_nontemporal_load(base + from + at[u]);
+#pragma unroll
+      for (int u = 0; u < kForkWords; ++u)
+        if (in[u]) __builtin_nontemporal_store(v[u], base + to + at[u]);
+    }
   }
 }
 
 hipError_t launch_fork(const ForkArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(fork_kernel, dim3(a.pieces, a.n_fork, a.pools.n_pools + (a.with_tables ? 1 : 0)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(fork_kernel, dim3(a.pieces, a.n_fork, a.shares + (a.with_tables ? 1 : 0)), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
