@@ -309,10 +309,15 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
   if (!aligned16(d_q) || !aligned16(d_out)) return fail(HC_EALIGN, "queries or output not 16-byte aligned");
   if (n_seq > 65535) return fail(HC_ERANGE, "at most 65535 contexts");
   if ((int64_t)h_total_q * d.n_q_heads > INT_MAX) return fail(HC_ERANGE, "total_q * n_q_heads must stay below 2^31");
-  const AttendPlan plan = plan_attend(d.n_q_heads, d.n_kv_heads, d.head_dim, n_seq, h_total_q, h_max_q, h_max_kv);
+  AttendPlan plan = plan_attend(d.n_q_heads, d.n_kv_heads, d.head_dim, n_seq, h_total_q, h_max_q, h_max_kv);
   if (plan.workspace) {
     if (!d_workspace || workspace_bytes < plan.workspace) return fail(HC_EINVAL, "workspace smaller than hc_attend_kv4_workspace says");
     if (!aligned16(d_workspace)) return fail(HC_EALIGN, "workspace not 16-byte aligned");
+  }
+  if (window > 0) {       // a window leaves fewer keys to share than the sizes say; the workspace is that of all keys
+    const int n_split = plan.n_split;
+    plan = plan_attend(d.n_q_heads, d.n_kv_heads, d.head_dim, n_seq, h_total_q, h_max_q, (int)std::min<int64_t>(h_max_kv, (int64_t)window + h_max_q));
+    plan.n_split = std::min(plan.n_split, n_split);
   }
   OnDevice on(ctx);
   HC_HIP(on.err);

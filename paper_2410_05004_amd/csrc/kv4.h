@@ -69,7 +69,7 @@ struct AttendPlan {
 };
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv);
 bool attend_head_dim(int head_dim);
-int attend_rows_blocks(int head_dim);      // row blocks of a workgroup of launch_attend_rows
+int attend_rows_blocks(int head_dim);      // row blocks of a workgroup of launch_attend_rows, which takes heads of 64 and 128
 hipError_t launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_attend(const AttendArgs& a, int head_dim, int row_blocks, hipStream_t stream);
 

@@ -13,20 +13,23 @@
 // several would store alike they all do.
 // Decoded keys and values are exact in bf16; W is rounded to bf16 (2^-9 relative, without a bias, which averages out over
 // the keys), sums and statistics are fp32.
+#include <algorithm>
+
 #include "kv4_device.h"
 
 namespace hc {
 
 // Rows of a context and KV head: row r is query r / group, query head r % group of the KV head's.  A workgroup takes
-// NB blocks of 16 rows and a share of the keys; its four waves take every fourth step of 32 keys, for all the rows.
+// NB blocks of 16 rows and a share of the keys; its waves take every so-many-th step of 32 keys, for all the rows.
 // The next step's bytes are fetched into the registers as soon as this step's are decoded: keys before the softmax, values
 // behind the second product.
+constexpr int kFewWaves = 4;
 template <int HD, int NB>
-__global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) void attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) void attend_kernel(const AttendArgs a) {
   constexpr int kSteps = HD / 32;         // matrix ops along the channels
   constexpr int kSlices = HD / 16;        // blocks of 16 channels of the result
-  __shared__ float s_out[3][kSlices * 4][64];
-  __shared__ float s_top[4][NB][16], s_sum[4][NB][16];
+  __shared__ float s_out[kFewWaves / 2][kSlices * 4][64];
+  __shared__ float s_top[kFewWaves][NB][16], s_sum[kFewWaves][NB][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q4 = lane >> 4;
   const int split = blockIdx.x % a.n_split, kvh = blockIdx.x / a.n_split, seq = blockIdx.z;
   int q0 = uniform(a.cu_q)[seq], q1 = uniform(a.cu_q)[seq + 1];
@@ -55,7 +58,7 @@ __global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) v
       const int r = (tile * NB + nb) * 16 + l16;
       return kvh * a.group + (r < n_rows ? r : n_rows - 1) - query * a.group;
     };
-    const int lane_key = (lane >> 1) * 128 + (lane & 1) * 16;        // run i of a round: half i % 2 of this wave's step i / 2
+    const int lane_key = (lane >> 1) * 32 * kFewWaves + (lane & 1) * 16;        // run i of a round: half i % 2 of this wave's step i / 2
     int first = 0, n_step = (keys + 31) >> 5, share = 0, step = 0, stop = 0;
     auto take_share = [&]() __attribute__((always_inline)) {
       share = (n_step + a.n_split - 1) / a.n_split;
@@ -92,6 +95,7 @@ __global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) v
       n_step = begin < end ? ((end + 31) >> 5) - first : 0;
       take_share();
     }
+    stop = min_of(stop, (end + 31) >> 5);
 
     f32x4 o[NB][kSlices];
     float top[NB], used[NB], sum[NB];                // used: the top, 0 while there is no finite one, so that exp2 of -inf stays 0
@@ -109,7 +113,7 @@ __global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) v
     auto next_runs = [&](int s) __attribute__((always_inline)) {       // places of step s
       if (at == 0) {
         places.settle(s * 32 + lane_key);
-        places.look_up((s + 128) * 32 + lane_key);
+        places.look_up((s + 32 * kFewWaves) * 32 + lane_key);
       }
       next_gone = ~(int)(places.there >> at) & 3;
     };
@@ -122,10 +126,10 @@ __global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) v
       }
       at = 2;
     }
-    for (; step < stop; step += 4) {
+    for (; step < stop; step += kFewWaves) {
       const int key0 = step * 32;
       gone = next_gone;
-      next_runs(step + 4);                           // behind the last step: some page's, not used
+      next_runs(step + kFewWaves);                           // behind the last step: some page's, not used
       const uint8_t* next_at[2] = {places.of(at), places.of(at + 1)};
       at = (at + 2) & 63;
       // ---- S^T = K Q^T
@@ -230,7 +234,7 @@ __global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) v
       for (int h = 0; h < 2; ++h) rv[h].load(next_at[h], l16, q4);
     }
 
-    // ---- the four waves' shares, added up in the waves' order; a block's results are one wave's to write
+    // ---- the waves' shares, added up by halves: an order that is always the same
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       sum[nb] = across_quarters(sum[nb], [](float p, float r) { return p + r; });
@@ -238,47 +242,57 @@ __global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) v
       s_sum[wave][nb][l16] = sum[nb];
     }
     __syncthreads();
+    float best[NB], total[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int writer = nb & 3;
-      float best = kNegInf;
+      best[nb] = kNegInf;
+      total[nb] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) best = fmaxf(best, s_top[i][nb][l16]);
-      const float best_used = best == kNegInf ? 0.f : best;
+      for (int i = 0; i < kFewWaves; ++i) best[nb] = fmaxf(best[nb], s_top[i][nb][l16]);
+      const float best_used = best[nb] == kNegInf ? 0.f : best[nb];
+#pragma unroll
+      for (int i = 0; i < kFewWaves; ++i) total[nb] += s_sum[i][nb][l16] * __builtin_amdgcn_exp2f(s_top[i][nb][l16] - best_used);
       const float mine = __builtin_amdgcn_exp2f(top[nb] - best_used);
 #pragma unroll
       for (int b = 0; b < kSlices; ++b) o[nb][b] *= mine;
-      if (wave != writer) {
-        const int at = wave - (wave > writer ? 1 : 0);
 #pragma unroll
-        for (int b = 0; b < kSlices; ++b)
+      for (int n = kFewWaves / 2; n > 0; n >>= 1) {
+        if (wave >= n && wave < 2 * n) {
 #pragma unroll
-          for (int v = 0; v < 4; ++v) s_out[at][b * 4 + v][lane] = o[nb][b][v];
+          for (int b = 0; b < kSlices; ++b)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) s_out[wave - n][b * 4 + v][lane] = o[nb][b][v];
+        }
+        __syncthreads();
+        if (wave < n) {
+#pragma unroll
+          for (int b = 0; b < kSlices; ++b)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[nb][b][v] += s_out[wave][b * 4 + v][lane];
+        }
+        __syncthreads();
       }
-      __syncthreads();
-      if (wave == writer && (tile * NB + nb) * 16 < n_rows) {       // places behind the last row have computed that row too and store the same
-        float total = 0.f;
+    }
+    if (wave == 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) total += s_sum[i][nb][l16] * __builtin_amdgcn_exp2f(s_top[i][nb][l16] - best_used);
+      for (int nb = 0; nb < NB; ++nb) {
+        if ((tile * NB + nb) * 16 >= n_rows) continue;       // places behind the last row have computed that row too and store the same
         const int qi = query_of(nb), head = head_of(nb, qi);
         const int64_t tok = q0 + qi, row = tok * a.n_q + head;
         // register (b, v) is channel (4 * q4 + v) * HD / 16 + b
-        auto joined = [&](int b, int v) __attribute__((always_inline)) {
-          return ((s_out[0][b * 4 + v][lane] + s_out[1][b * 4 + v][lane]) + s_out[2][b * 4 + v][lane]) + o[nb][b][v];
-        };
         if (a.n_split == 1) {
-          const float norm = total == 0.f ? 0.f : 1.f / total;         // a row that sees no key: zeros
+          const float norm = total[nb] == 0.f ? 0.f : 1.f / total[nb];         // a row that sees no key: zeros
           uint16_t* to = a.out + tok * a.out_stride + head * HD + q4 * (HD / 4);
 #pragma unroll
           for (int v = 0; v < 4; ++v)
 #pragma unroll
             for (int b = 0; b < kSlices; b += 4) {
               u32x2 y;
-              y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{joined(b, v) * norm, joined(b + 1, v) * norm}, bf16x2));
-              y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{joined(b + 2, v) * norm, joined(b + 3, v) * norm}, bf16x2));
+              y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[nb][b][v] * norm, o[nb][b + 1][v] * norm}, bf16x2));
+              y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[nb][b + 2][v] * norm, o[nb][b + 3][v] * norm}, bf16x2));
               *reinterpret_cast<u32x2*>(to + v * kSlices + b) = y;
             }
-          if (a.lse) a.lse[row] = best_used * 0.69314718056f + __logf(total);
+          if (a.lse) a.lse[row] = (best[nb] == kNegInf ? 0.f : best[nb]) * 0.69314718056f + __logf(total[nb]);
         } else {
           const int64_t n_row = (int64_t)a.total_q * a.n_q;
           float* to = a.part + (split * n_row + row) * HD + q4 * (HD / 4);
@@ -286,12 +300,12 @@ __global__ __launch_bounds__(256, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) v
           for (int v = 0; v < 4; ++v)
 #pragma unroll
             for (int b = 0; b < kSlices; b += 4)
-              *reinterpret_cast<f32x4*>(to + v * kSlices + b) = f32x4{joined(b, v), joined(b + 1, v), joined(b + 2, v), joined(b + 3, v)};
-          *reinterpret_cast<f32x2*>(a.part + a.n_split * n_row * HD + (split * n_row + row) * 2) = f32x2{best, total};
+              *reinterpret_cast<f32x4*>(to + v * kSlices + b) = f32x4{o[nb][b][v], o[nb][b + 1][v], o[nb][b + 2][v], o[nb][b + 3][v]};
+          *reinterpret_cast<f32x2*>(a.part + a.n_split * n_row * HD + (split * n_row + row) * 2) = f32x2{best[nb], total[nb]};
         }
       }
-      __syncthreads();
     }
+    __syncthreads();
   }
   if (bad_page && lane == 0) atomicOr(a.err, HC_DEV_BAD_PAGE);
 }
@@ -351,25 +365,53 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
 
 bool attend_head_dim(int head_dim) { return head_dim == 64 || head_dim == 128 || head_dim == 256; }
 
-// Blocks of 16 rows of a workgroup.
-static int row_blocks(int head_dim, int64_t rows) {
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : attend_rows_blocks(head_dim);
+// Blocks of 16 rows of a workgroup, for `rows` of the longest context, `blocks` of 16 in all contexts and KV heads and as many `tiles`
+// of kv4_prompt.hip's workgroups.
+// Measured, 32 heads of 128 over 8 KV heads unless said otherwise, microseconds with 1 | 2 blocks | that kernel:
+// - one context, 16 queries, 1000 keys 10.2 | 12.8, 64 queries, 1000 keys 10.2 | 12.9, 256 queries, 1000 keys 13.2 | 13.3; 64 queries,
+//   8000 keys 27.8 | 25.6; 1024 queries, 16000 keys 392 | 307; 14 heads of 64 over 2, 64 queries, 8000 keys 15.1 | 15.0, 1024 queries,
+//   4000 keys 41 | 32: keys are decoded once for 32 rows, and half as many waves wait for memory at once, so 2 blocks from some
+//   800 000 pairs of a block and a key on (64 contexts of 4 queries, 2000 keys 23 | 27: not for 16 rows).  256 channels take registers
+//   for one wave of a SIMD then: 16 heads over 8, 64 queries, 8000 keys 31 | 48, 8 contexts of 1024, 2048 keys 296 | 448 | 322: always 1.
+// - kv4_prompt.hip decodes for 128 or 256 rows, but starts late (30 us with next to no keys) and has two workgroups on a compute unit:
+//   8 contexts of 256 queries, 1000 keys 50 | 49 | 38; of 64 queries, 4000 keys 45 | 39 | 50; of 1024 queries, 2048 keys 298 | 247 | 205;
+//   64 of 128 queries, 4000 keys 576 | 469 | 397; one of 1024, 1024 keys 27 | 26 | 33, 4000 keys 100 | 77 | 87, 16000 keys
+//   392 | 307 | 277; one of 256, 16000 keys 118 | 102 | 93; 64 of 16 (64 rows) 55 | 48 | 65: if its tiles are filled to three quarters,
+//   and there are two for every compute unit, or fewer than one and keys enough for shares of 1024 at least.
+static int row_blocks(int head_dim, int64_t rows, int64_t blocks, int64_t keys, int64_t tiles, bool filled) {
+  const bool wide = head_dim == 256;
+  if (!wide && filled && (tiles >= 2 * kChipCUs || (tiles <= kChipCUs && keys >= 8192 && tiles * keys >= 2 * kChipCUs * 1024)))
+    return attend_rows_blocks(head_dim);
+  return !wide && rows > 16 && blocks * keys >= 3 << 18 ? 2 : 1;
+}
+
+// Shares of the keys, of `base` workgroups without any.  A second share costs a launch that joins (3 us, and as much on the host)
+// and every workgroup a start of several dependent loads, so: none up to 1280 keys (8 KV heads, one context: 1000 keys 10.1 us
+// whole, 9.5 shared; 2000 keys 15.0 and 9.7); up to a workgroup on each compute unit shares of 128 keys, up to two of 512 (16000
+// keys: 13.8 us in 128 workgroups, 12.1 in 256, 12.8 in 512), beyond that, where contexts are uneven and the last ones
+// would run alone, of 2048 (64 contexts of up to 8192 keys: 109 us in 512 workgroups, 89 in 2048; of up to 4000: 41 and 44), but not
+// for contexts of several workgroups, whose results are more to join (64 queries, 32000 keys: 59 us in 960 workgroups, 53 in 512).
+static int key_shares(int64_t base, int64_t keys, bool one_tile) {
+  if (base <= 0 || keys <= 1280) return 1;
+  int64_t n = std::min<int64_t>(kChipCUs / base, keys / 128);
+  n = std::max(n, std::min<int64_t>(2 * kChipCUs / base, keys / 512));
+  if (one_tile) n = std::max(n, std::min<int64_t>(8 * kChipCUs / base, keys / 2048));
+  return (int)std::max<int64_t>(n, 1);
 }
 
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv) {
   AttendPlan p;
-  const int64_t rows = (int64_t)max_q * (n_q / n_kv);
-  p.row_blocks = row_blocks(head_dim, rows);
-  const int64_t tiles = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);
-  p.row_tiles = (int)(tiles < 1 ? 1 : tiles > 65535 ? 65535 : tiles);
-  const int64_t base = (int64_t)n_seq * n_kv * p.row_tiles;
-  // Keys are split until the chip is full: two workgroups a compute unit for prompts and for a context alone, whose shares are
-  // alike, more where contexts differ, so that none of them is long at the end (64 contexts of 2K to 8K keys: 99 us in 1024
-  // workgroups, 89 in 2048, 91 to 99 in 4096; one of 128K keys: 33 us in 2048, 27 in 512); not below 256 keys to one.
-  const int64_t wanted = p.row_blocks > 2 || n_seq == 1 ? 2 * kChipCUs : 8 * kChipCUs;
-  int64_t split = base > 0 ? wanted / base : 1, most = ((int64_t)max_kv + 255) / 256;
-  if (split > most) split = most;
-  p.n_split = split < 1 ? 1 : (int)split;
+  const int64_t group = n_q / n_kv, rows = std::max<int64_t>((int64_t)max_q * group, 1), all_rows = (int64_t)total_q * group;
+  // tiles of `size` rows of all contexts and KV heads: the longest context is one of n_seq, and none has less than one tile
+  auto tiles_of = [&](int64_t size) {
+    const int64_t each = (rows + size - 1) / size;
+    return n_kv * std::min<int64_t>(n_seq * each, std::max<int64_t>(n_seq, (all_rows + size - 1) / size));
+  };
+  const int64_t many = 16 * attend_rows_blocks(head_dim);
+  p.row_blocks = row_blocks(head_dim, rows, tiles_of(16), max_kv, tiles_of(many), 4 * rows >= 3 * ((rows + many - 1) / many) * many);
+  const int64_t size = 16 * p.row_blocks;
+  p.row_tiles = (int)std::min<int64_t>((rows + size - 1) / size, 65535);
+  p.n_split = key_shares(tiles_of(size), max_kv, p.row_tiles == 1 && p.row_blocks <= 2);
   p.workspace = p.n_split > 1 ? (int64_t)p.n_split * total_q * n_q * (head_dim + 2) * 4 : 0;
   return p;
 }
@@ -377,9 +419,13 @@ AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, 
 template <int HD>
 static void launch_hd(const AttendArgs& a, int row_blocks, hipStream_t stream) {
   const dim3 grid(a.n_split * a.n_kv, a.row_tiles, a.n_seq);
-  if (row_blocks == 1)      hipLaunchKernelGGL((attend_kernel<HD, 1>), grid, dim3(256), 0, stream, a);
-  else if (row_blocks == 2) hipLaunchKernelGGL((attend_kernel<HD, 2>), grid, dim3(256), 0, stream, a);
-  else                      (void)launch_attend_rows(a, HD, stream);
+  if (row_blocks > 2) {
+    (void)launch_attend_rows(a, HD, stream);
+  } else if (row_blocks == 1) {
+    hipLaunchKernelGGL((attend_kernel<HD, 1>), grid, dim3(64 * kFewWaves), 0, stream, a);
+  } else if constexpr (HD <= 128) {
+    hipLaunchKernelGGL((attend_kernel<HD, 2>), grid, dim3(64 * kFewWaves), 0, stream, a);
+  }
   if (a.n_split > 1) {
     const int64_t n_row = (int64_t)a.total_q * a.n_q;
     if (a.n_split <= 4) hipLaunchKernelGGL((attend_join_kernel<HD, 4>), dim3((unsigned)((n_row + 3) / 4)), dim3(256), 0, stream, a);

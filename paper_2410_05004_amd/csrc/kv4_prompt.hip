@@ -1,5 +1,5 @@
 // Attention of many rows over the 4-bit cache: prompts on histories.  The mathematics and the matrix ops' operands are
-// those of kv4_attend.hip; here a decoded key or value serves 64 * NB rows of a workgroup instead of 16 * NB.
+// those of kv4_attend.hip; here a decoded key or value serves 128 * NB rows of a workgroup instead of 16 * NB.
 #include "kv4_device.h"
 
 namespace hc {
@@ -10,7 +10,7 @@ namespace hc {
 // As K's rows lane (l32, half) takes key l32 and, in step j, channels (2 * (j / n) + half) * HD / 4 + j % n * 8 .. + 7, n = HD / 32; as
 // V^T's rows channels of slice l32 % 16, the even or the odd one of pair c.
 template <int HD, int NB>       // NB: blocks of 32 rows of a wave
-__global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a) {
   constexpr int kSteps = HD / 16, kBlocks = HD / 32, kTile = 64, kWaves = 4;       // matrix ops along the channels; blocks of 32 channels of the result
   __shared__ u32x4 s_k[2][2][kSteps][64], s_v[2][2][2][kBlocks][64];
   __shared__ int s_range[kWaves][4], s_nan[2];
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(con
     auto decode_keys = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j) {
-        const float ks = scale_of(rk.scales, HD == 256 ? j >> 2 : 0);
+        const float ks = scale_of(rk.scales, 0);
         u32x4 k;
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[i] = decode2(rk.w[j], ks, i);
@@ -223,17 +223,14 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(con
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u) {
+            // registers 4 * u + i and 8 + 4 * u + i, i < 4, are channels of slices 8 * u + 4 * half + i, of one group of 32
+            const float poison = nan_values<HD>(places, key0, 32, lo[nb], hi[nb], (8 * u + 4 * half) * HD / 512);
 #pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-              // registers 8 * odd + 4 * u + i are channels of slice 8 * u + 4 * half + i: a group of 32, HD = 256 two
-              const int group = (8 * u + 4 * half + i) * HD / 512;
-              const float poison = nan_values<HD>(places, key0, 32, lo[nb], hi[nb], group);
+            for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
-              for (int c = 0; c < kBlocks; ++c)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o[nb][c][8 * (x >> 1) + 4 * u + i + (x & 1)] += poison;
-            }
+              for (int x = 0; x < 8; ++x) o[nb][c][8 * (x >> 2) + 4 * u + (x & 3)] += poison;
+          }
       }
     };
 
@@ -334,18 +331,15 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(con
   if (bad_page && lane == 0) atomicOr(a.err, HC_DEV_BAD_PAGE);
 }
 
-// blocks of 32 rows of a wave: as many as leave room for two waves in a SIMD's registers (256 channels: for one)
+// blocks of 32 rows of a wave: as many as leave room for two waves in a SIMD's registers
 constexpr int wave_blocks(int head_dim) { return head_dim == 64 ? 2 : 1; }
 
 int attend_rows_blocks(int head_dim) { return 8 * wave_blocks(head_dim); }
 
 hipError_t launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream) {
   const dim3 grid(a.n_split * a.n_kv, a.row_tiles, a.n_seq);
-  switch (head_dim) {
-    case 64: hipLaunchKernelGGL((attend_rows_kernel<64, wave_blocks(64)>), grid, dim3(256), 0, stream, a); break;
-    case 128: hipLaunchKernelGGL((attend_rows_kernel<128, wave_blocks(128)>), grid, dim3(256), 0, stream, a); break;
-    default: hipLaunchKernelGGL((attend_rows_kernel<256, wave_blocks(256)>), grid, dim3(256), 0, stream, a); break;
-  }
+  if (head_dim == 64) hipLaunchKernelGGL((attend_rows_kernel<64, wave_blocks(64)>), grid, dim3(256), 0, stream, a);
+  else                hipLaunchKernelGGL((attend_rows_kernel<128, wave_blocks(128)>), grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

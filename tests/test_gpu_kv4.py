@@ -392,3 +392,83 @@ def test_two_at_once(hc, torch):
     torch.cuda.synchronize()
     for c, (o, l) in zip(calls, want):
         assert torch.equal(c.out, o) and torch.equal(c.lse, l)
+
+
+# ---- every way that sizes lead to: a workgroup of 16 rows, of 32, of 128 or 256, each with all of the keys or a share of them.  The sizes
+# that a caller states are upper bounds; stated wider than they are, they lead small contexts there too.
+WAYS = ["few", "few-shared", "few-halved", "two", "two-shared", "many", "many-shared"]
+SHAPES = [(4, 4, 64, 16), (8, 2, 128, 16), (14, 2, 64, 32), (5, 5, 128, 64), (34, 1, 64, 16), (6, 2, 128, 32)]
+
+
+def stated(way, n_q, n_kv, hd):
+    """Contexts to fill up to with empty ones, queries of the longest, keys of the longest."""
+    full, two = (256 if hd == 64 else 128) * n_kv // n_q, 32 * n_kv // n_q
+    return {"few": (0, 1, 1), "few-shared": (0, 1, 4000), "few-halved": (-(-150 // n_kv), 1, 4000), "two": (-(-640 // n_kv), max(two, 1), 1280),
+            "two-shared": (0, max(two, 1), 1 << 20), "many": (-(-512 // n_kv), full, 1000), "many-shared": (0, full, 1 << 20)}[way]
+
+
+def call_by(way, hc, rng, lens, q_lens, n_q, n_kv, hd, block, **more):
+    n, max_q, max_kv = stated(way, n_q, n_kv, hd)
+    empty = [0] * max(0, n - len(lens))
+    return Call(hc, rng, kh.Cache(rng, lens + empty, n_kv, hd, block), n_q, q_lens + empty, max_q=max_q, max_kv=max_kv, **more)
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("n_q,n_kv,hd,block", SHAPES)
+def test_ways(hc, way, n_q, n_kv, hd, block):
+    rng = np.random.default_rng([21, n_q, hd])
+    lens, q_lens = [50, 7, 130, 300, 20, 1], [50, 9, 1, 77, 0, 1]
+    call = call_by(way, hc, rng, lens, q_lens, n_q, n_kv, hd, block, pad=8, q_extra=16, extra_rows=3)
+    assert (call.ws.numel() > 0) == (way.endswith("shared") or way == "few-halved")
+    out = call.check()
+    assert np.all(out[50:52] == 0)
+
+
+@pytest.mark.parametrize("window", [1, 37, 2 ** 31 - 1])
+@pytest.mark.parametrize("n_q,n_kv,hd,block", SHAPES)
+def test_windows_of_many_rows(hc, n_q, n_kv, hd, block, window):
+    rng = np.random.default_rng([22, n_q, hd, window])
+    call_by("many", hc, rng, [50, 7, 130, 500, 20], [50, 9, 1, 300, 0], n_q, n_kv, hd, block, window=window).check()
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("n_q,n_kv,hd,block", [(2, 2, 64, 16), (4, 2, 128, 16)])
+def test_ways_with_nan_and_missing_pages(hc, way, n_q, n_kv, hd, block):
+    rng = np.random.default_rng([23, hd])
+    call = call_by(way, hc, rng, [100, 300], [40, 200], n_q, n_kv, hd, block)
+    cache = call.cache
+    for part, s, head, key, group in ((1, 0, n_kv - 1, 80, 1), (1, 1, 0, 261, hd // 32 - 1), (0, 1, 0, 295, 0), (1, 1, 1, 101, 0)):
+        page, slot = cache.tables[s, key // 16], key % 16
+        cache.pool[page, head, 0][kv4.places(part, head, slot, hd)[2][group]] = 255
+    call.pool.copy_(kh.dev_u8(cache.pool))
+    out = call.check()
+    assert np.isnan(out).any() and not np.isnan(out).all()
+    cache.tables[0, 2], cache.tables[1, 15], cache.tables[1, 0] = -1, cache.num_pages, 1 << 30
+    call.d["tab"].copy_(gh.to_dev_i32(cache.tables))
+    call.check(flags=hc.HC_DEV_BAD_PAGE)
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_ways_with_positions_in_any_order(hc, way):
+    rng = np.random.default_rng(24)
+    pos = np.concatenate([[5, 2 ** 31 - 1, -1, 299, 0, 5, 300, 40, -2 ** 31, 63, 62, 64, 298, 1], rng.integers(-5, 320, 186)])
+    for scale, q_scale in ((None, 1.0), (3.0, 4.0)):
+        out = call_by(way, hc, rng, [300], [200], 4, 2, 128, 16, positions=pos, scale=scale, q_scale=q_scale).check()
+        assert np.all(out[[2, 8]] == 0)
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_ways_in_a_graph(hc, torch, way):
+    rng = np.random.default_rng(25)
+    call = call_by(way, hc, rng, [700, 90], [300, 3], 8, 2, 128, 16)
+    want = torch.from_numpy(call.check()).cuda()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call.launch(stream=side.cuda_stream)
+    for _ in range(3):
+        call.out.fill_(99)
+        call.ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(call.out.double().view(want.shape), want)
