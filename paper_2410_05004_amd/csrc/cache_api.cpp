@@ -345,7 +345,8 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
   a.group = d.n_q_heads / d.n_kv_heads;
   a.window = window;
   a.scale_log2 = scale * 1.44269504089f;
-  a.row_tiles = plan.row_tiles;
+  a.flat = plan.flat;
+  a.n_slots = plan.n_slots;
   a.n_split = plan.n_split;
   HC_HIP(launch_attend(a, d.head_dim, plan.row_blocks, static_cast<hipStream_t>(stream)));
   return HC_OK;

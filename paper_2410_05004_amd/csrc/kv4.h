@@ -60,17 +60,23 @@ struct AttendArgs {
   int32_t n_q, n_kv, group;                // query heads, KV heads, query heads of one KV head
   int32_t window;                          // 0: none
   float scale_log2;                        // softmax scale * log2(e)
-  int32_t row_tiles, n_split;
+  int32_t flat, n_slots, n_split;          // see AttendPlan
 };
 struct AttendPlan {
   int32_t row_blocks;                      // blocks of 16 rows of a workgroup; kv4_prompt.hip from 8 on
-  int32_t row_tiles, n_split;              // workgroups along a context's rows, shares of the keys
+  // Places for workgroups along the rows, of a KV head and share of the keys: one a context, which goes through all of its tiles of rows
+  // (one, if the sizes are right); or, flat, one a tile: context s has those from cu[s] * group / size + s on, up to one too many.
+  int32_t flat, n_slots, n_split;
   int64_t workspace;                       // bytes
 };
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv);
 bool attend_head_dim(int head_dim);
 int attend_rows_blocks(int head_dim);      // row blocks of a workgroup of launch_attend_rows, which takes heads of 64 and 128
-hipError_t launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream);
+inline dim3 attend_grid(const AttendArgs& a) {      // places over two dimensions of less than 65536
+  const int y = a.n_slots < 32768 ? a.n_slots : 32768;
+  return dim3(a.n_split * a.n_kv, y, (a.n_slots + y - 1) / y);
+}
+void launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_attend(const AttendArgs& a, int head_dim, int row_blocks, hipStream_t stream);
 
 }  // namespace hc

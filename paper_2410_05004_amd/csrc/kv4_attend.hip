@@ -31,23 +31,20 @@ __global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256
   __shared__ float s_out[kFewWaves / 2][kSlices * 4][64];
   __shared__ float s_top[kFewWaves][NB][16], s_sum[kFewWaves][NB][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q4 = lane >> 4;
-  const int split = blockIdx.x % a.n_split, kvh = blockIdx.x / a.n_split, seq = blockIdx.z;
-  int q0 = uniform(a.cu_q)[seq], q1 = uniform(a.cu_q)[seq + 1];
-  q0 = q0 < 0 ? 0 : q0;
-  q1 = q1 > a.total_q ? a.total_q : q1;
+  const int split = blockIdx.x % a.n_split, kvh = blockIdx.x / a.n_split;
+  const Task task(a, NB * 16);
+  const int seq = task.seq, q0 = task.q0, n_rows = task.n_rows;
   const int64_t room = (int64_t)a.max_blocks << a.block_shift, most = room < kMaxKeys ? room : kMaxKeys;
   int keys = uniform(a.kv_lens)[seq];
   if (keys > most || keys < 0) {
     if (threadIdx.x == 0) atomicOr(a.err, HC_DEV_BAD_POSITION);
     keys = keys < 0 ? 0 : (int)most;
   }
-  const int n_rows = (q1 - q0) * a.group, n_tiles = (n_rows + NB * 16 - 1) / (NB * 16);
+  if (task.tile < 0) return;                         // not before the count is asked for: both are on their way together
   Places places(a, seq, kvh, sub_bytes(HD));
   bool bad_page = false;
 
-  // the last rows first: they see the most keys
-  for (int turn = blockIdx.y; turn < n_tiles; turn += gridDim.y) {
-    const int tile = n_tiles - 1 - turn;
+  for (int tile = task.tile; tile >= 0; tile -= task.step) {
     // ---- this workgroup's share of the keys, in steps of 32: of all that there are, or, if there is a window, of those that any row
     // sees.  Without one nothing waits for the positions: the table's entries and the rows are on their way together.
     auto query_of = [&](int nb) __attribute__((always_inline)) {
@@ -140,7 +137,7 @@ __global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256
         for (int nb = 0; nb < NB; ++nb) s[nb][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-          const float ks = scale_of(rk[h].scales, HD == 256 ? j >> 2 : 0);
+          const float ks = rk[h].scale(l16, q4, j);
           u32x4 k;
 #pragma unroll
           for (int i = 0; i < 4; ++i) k[i] = decode2(rk[h].w[j], ks, i);
@@ -365,8 +362,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
 
 bool attend_head_dim(int head_dim) { return head_dim == 64 || head_dim == 128 || head_dim == 256; }
 
-// Blocks of 16 rows of a workgroup, for `rows` of the longest context, `blocks` of 16 in all contexts and KV heads and as many `tiles`
-// of kv4_prompt.hip's workgroups.
+// Blocks of 16 rows of a workgroup, for `blocks` of them in all contexts and KV heads and `tiles` of kv4_prompt.hip's workgroups.
+// `some`: contexts have more than one block; `filled`: they fill those tiles.
 // Measured, 32 heads of 128 over 8 KV heads unless said otherwise, microseconds with 1 | 2 blocks | that kernel:
 // - one context, 16 queries, 1000 keys 10.2 | 12.8, 64 queries, 1000 keys 10.2 | 12.9, 256 queries, 1000 keys 13.2 | 13.3; 64 queries,
 //   8000 keys 27.8 | 25.6; 1024 queries, 16000 keys 392 | 307; 14 heads of 64 over 2, 64 queries, 8000 keys 15.1 | 15.0, 1024 queries,
@@ -378,11 +375,11 @@ bool attend_head_dim(int head_dim) { return head_dim == 64 || head_dim == 128 ||
 //   64 of 128 queries, 4000 keys 576 | 469 | 397; one of 1024, 1024 keys 27 | 26 | 33, 4000 keys 100 | 77 | 87, 16000 keys
 //   392 | 307 | 277; one of 256, 16000 keys 118 | 102 | 93; 64 of 16 (64 rows) 55 | 48 | 65: if its tiles are filled to three quarters,
 //   and there are two for every compute unit, or fewer than one and keys enough for shares of 1024 at least.
-static int row_blocks(int head_dim, int64_t rows, int64_t blocks, int64_t keys, int64_t tiles, bool filled) {
+static int row_blocks(int head_dim, int64_t blocks, int64_t keys, int64_t tiles, bool some, bool filled) {
   const bool wide = head_dim == 256;
   if (!wide && filled && (tiles >= 2 * kChipCUs || (tiles <= kChipCUs && keys >= 8192 && tiles * keys >= 2 * kChipCUs * 1024)))
     return attend_rows_blocks(head_dim);
-  return !wide && rows > 16 && blocks * keys >= 3 << 18 ? 2 : 1;
+  return !wide && some && blocks * keys >= 3 << 18 ? 2 : 1;
 }
 
 // Shares of the keys, of `base` workgroups without any.  A second share costs a launch that joins (3 us, and as much on the host)
@@ -402,25 +399,31 @@ static int key_shares(int64_t base, int64_t keys, bool one_tile) {
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv) {
   AttendPlan p;
   const int64_t group = n_q / n_kv, rows = std::max<int64_t>((int64_t)max_q * group, 1), all_rows = (int64_t)total_q * group;
-  // tiles of `size` rows of all contexts and KV heads: the longest context is one of n_seq, and none has less than one tile
-  auto tiles_of = [&](int64_t size) {
-    const int64_t each = (rows + size - 1) / size;
-    return n_kv * std::min<int64_t>(n_seq * each, std::max<int64_t>(n_seq, (all_rows + size - 1) / size));
-  };
+  // tiles of `size` rows of all contexts and KV heads, about
+  auto tiles_of = [&](int64_t size) { return n_kv * std::max<int64_t>(n_seq, (all_rows + size - 1) / size); };
   const int64_t many = 16 * attend_rows_blocks(head_dim);
-  p.row_blocks = row_blocks(head_dim, rows, tiles_of(16), max_kv, tiles_of(many), 4 * rows >= 3 * ((rows + many - 1) / many) * many);
+  // Among contexts of other sizes than the longest's, single tokens mostly, wide workgroups are wasted: 512 queries on 512 keys and 63 times
+  // one on 2000, 14 heads of 64 over 2, 15 us with 1 block, 20 with 2, 37 in kv4_prompt.hip; 32 heads of 128 over 8, 2048 queries twice and
+  // 200 times one 208, 184, 206, 8192 queries and 255 times one 999, 774, 821, and 63 times one 904, 671, 606.
+  const bool even = 2 * (int64_t)total_q >= (int64_t)n_seq * max_q;
+  const bool filled = 4 * rows >= 3 * ((rows + many - 1) / many) * many && all_rows >= (even ? 3 * many / 4 : 8 * many) * n_seq;
+  const bool some = rows > 16 && (even || all_rows >= 64 * (int64_t)n_seq);
+  p.row_blocks = row_blocks(head_dim, tiles_of(16), max_kv, tiles_of(many), some, filled);
   const int64_t size = 16 * p.row_blocks;
-  p.row_tiles = (int)std::min<int64_t>((rows + size - 1) / size, 65535);
-  p.n_split = key_shares(tiles_of(size), max_kv, p.row_tiles == 1 && p.row_blocks <= 2);
+  // a place a tile: contexts of very different sizes then leave next to none empty (8192 queries and 255 times one: 774 us; with places
+  // for the longest in every context 1760)
+  p.flat = rows > size;
+  p.n_slots = (int)(p.flat ? all_rows / size + n_seq : n_seq);
+  p.n_split = key_shares(tiles_of(size), max_kv, !p.flat && p.row_blocks <= 2);
   p.workspace = p.n_split > 1 ? (int64_t)p.n_split * total_q * n_q * (head_dim + 2) * 4 : 0;
   return p;
 }
 
 template <int HD>
 static void launch_hd(const AttendArgs& a, int row_blocks, hipStream_t stream) {
-  const dim3 grid(a.n_split * a.n_kv, a.row_tiles, a.n_seq);
+  const dim3 grid = attend_grid(a);
   if (row_blocks > 2) {
-    (void)launch_attend_rows(a, HD, stream);
+    launch_attend_rows(a, HD, stream);
   } else if (row_blocks == 1) {
     hipLaunchKernelGGL((attend_kernel<HD, 1>), grid, dim3(64 * kFewWaves), 0, stream, a);
   } else if constexpr (HD <= 128) {

@@ -75,6 +75,39 @@ __device__ __forceinline__ int max_of(int a, int b) { return a > b ? a : b; }
 typedef const int32_t __attribute__((address_space(4)))* uniform_ints;
 __device__ __forceinline__ uniform_ints uniform(const int32_t* p) { return (uniform_ints)(uintptr_t)p; }
 
+// The context and the tile of `size` rows that a workgroup begins with, and how far down it goes on (AttendPlan).
+struct Task {
+  int seq, q0, q1, n_rows, tile, step;
+  static __device__ __forceinline__ int within(const AttendArgs& a, int q) { return q < 0 ? 0 : q > a.total_q ? a.total_q : q; }
+  __device__ __forceinline__ Task(const AttendArgs& a, int size) {
+    const int slot = blockIdx.z * gridDim.y + blockIdx.y;
+    seq = slot;
+    int before = 0;                                  // tiles of the context whose places come first: the last rows see the most keys
+    if (a.flat) {
+      // contexts 1 .. n_seq - 1 that begin at this place or before it, by 64 lanes at once
+      seq = 0;
+      for (int left = a.n_seq - 1; left > 0;) {
+        const int by = (left + 63) >> 6, s = seq + ((threadIdx.x & 63) + 1) * by;
+        const bool begun = s < a.n_seq && within(a, a.cu_q[s]) * a.group / size + s <= slot;
+        seq += __popcll(__ballot(begun)) * by;
+        left = by > 1 ? by : 0;
+      }
+      seq = __builtin_amdgcn_readfirstlane(seq);
+    }
+    if (seq < a.n_seq) {
+      q0 = within(a, uniform(a.cu_q)[seq]);
+      q1 = within(a, uniform(a.cu_q)[seq + 1]);
+      if (a.flat) before = slot - (q0 * a.group / size + seq);
+    } else {
+      seq = q0 = q1 = 0;
+    }
+    n_rows = (q1 - q0) * a.group;
+    const int n_tiles = n_rows > 0 ? (n_rows + size - 1) / size : 0;
+    tile = before < 0 ? -1 : n_tiles - 1 - before;
+    step = a.flat ? 0x40000000 : 1;                  // more than there are tiles
+  }
+};
+
 // Where runs of 16 keys of a KV head stand, 64 runs at a time: run i's offset is lane i's, worked out by all lanes at once (per
 // run and wave the 64-bit products would be some 25 scalar instructions), and the entries of the 64 behind are on their
 // way meanwhile.
@@ -146,15 +179,19 @@ __device__ __forceinline__ void load_words(uint32_t* to, const uint8_t* from) {
     }
   }
 }
+// K's scales as the word that they are in: of a byte the compiler would clear the other bits where the load is given its
+// place in the loop, and wait for it there (64 contexts of up to 8192 keys: 81 us without, 88 with that wait).
 template <int HD>
 struct RawK {
   uint32_t w[HD / 32], scales;
   __device__ __forceinline__ void load(const uint8_t* at, int l16, int q4) {
     load_words<HD / 32>(w, at + (l16 * (HD / 2) + q4 * (HD / 8)));
-    const uint8_t* s = at + (k_scales_at(HD) + l16 * (HD / 32));
-    if constexpr (HD == 64)       scales = s[q4 >> 1];
-    else if constexpr (HD == 128) scales = s[q4];
-    else                          scales = *reinterpret_cast<const uint16_t*>(s + 2 * q4);
+    scales = *reinterpret_cast<const uint32_t*>(at + k_scales_at(HD) + ((l16 * (HD / 32) + q4 * HD / 128) & ~3));
+  }
+  // scale of word j; the lane's first byte of the word goes to the exponent's place in one turn
+  __device__ __forceinline__ float scale(int l16, int q4, int j) const {
+    const uint32_t first = ((l16 * (HD / 32) + q4 * HD / 128) & 3) * 8 + 9;
+    return __uint_as_float(__builtin_rotateright32(scales, first + (HD == 256 ? 8 * (j >> 2) : 0)));
   }
 };
 template <int HD>

@@ -15,22 +15,21 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
   __shared__ u32x4 s_k[2][2][kSteps][64], s_v[2][2][2][kBlocks][64];
   __shared__ int s_range[kWaves][4], s_nan[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q4 = lane >> 4, l32 = lane & 31, half = lane >> 5;
-  const int split = blockIdx.x % a.n_split, kvh = blockIdx.x / a.n_split, seq = blockIdx.z;
-  int q0 = uniform(a.cu_q)[seq], q1 = uniform(a.cu_q)[seq + 1];
-  q0 = q0 < 0 ? 0 : q0;
-  q1 = q1 > a.total_q ? a.total_q : q1;
+  const int split = blockIdx.x % a.n_split, kvh = blockIdx.x / a.n_split;
+  const Task task(a, 32 * NB * kWaves);
+  const int seq = task.seq, q0 = task.q0, n_rows = task.n_rows;
   const int64_t room = (int64_t)a.max_blocks << a.block_shift, most = room < kMaxKeys ? room : kMaxKeys;
   int keys = uniform(a.kv_lens)[seq];
   if (keys > most || keys < 0) {
     if (threadIdx.x == 0) atomicOr(a.err, HC_DEV_BAD_POSITION);
     keys = keys < 0 ? 0 : (int)most;
   }
-  const int n_rows = (q1 - q0) * a.group, n_tiles = (n_rows + 32 * NB * kWaves - 1) / (32 * NB * kWaves);
+  if (task.tile < 0) return;                         // not before the count is asked for: both are on their way together
   Places places(a, seq, kvh, sub_bytes(HD));
   bool bad_page = false;
 
-  for (int turn = blockIdx.y; turn < n_tiles; turn += gridDim.y) {
-    const int block0 = ((n_tiles - 1 - turn) * kWaves + wave) * NB;        // this wave's first block of rows; the last rows first: they see the most keys
+  for (int tile_of_rows = task.tile; tile_of_rows >= 0; tile_of_rows -= task.step) {
+    const int block0 = (tile_of_rows * kWaves + wave) * NB;                // this wave's first block of rows
     auto row_of = [&](int nb) __attribute__((always_inline)) {
       const int r = (block0 + nb) * 32 + l32;
       return r < n_rows ? r : n_rows - 1;
@@ -107,7 +106,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
     auto decode_keys = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j) {
-        const float ks = scale_of(rk.scales, 0);
+        const float ks = rk.scale(l16, q4, j);
         u32x4 k;
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[i] = decode2(rk.w[j], ks, i);
@@ -336,11 +335,10 @@ constexpr int wave_blocks(int head_dim) { return head_dim == 64 ? 2 : 1; }
 
 int attend_rows_blocks(int head_dim) { return 8 * wave_blocks(head_dim); }
 
-hipError_t launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream) {
-  const dim3 grid(a.n_split * a.n_kv, a.row_tiles, a.n_seq);
+void launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream) {
+  const dim3 grid = attend_grid(a);
   if (head_dim == 64) hipLaunchKernelGGL((attend_rows_kernel<64, wave_blocks(64)>), grid, dim3(256), 0, stream, a);
   else                hipLaunchKernelGGL((attend_rows_kernel<128, wave_blocks(128)>), grid, dim3(256), 0, stream, a);
-  return hipGetLastError();
 }
 
 }  // namespace hc

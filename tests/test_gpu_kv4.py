@@ -396,21 +396,21 @@ def test_two_at_once(hc, torch):
 
 # ---- every way that sizes lead to: a workgroup of 16 rows, of 32, of 128 or 256, each with all of the keys or a share of them.  The sizes
 # that a caller states are upper bounds; stated wider than they are, they lead small contexts there too.
-WAYS = ["few", "few-shared", "few-halved", "two", "two-shared", "many", "many-shared"]
+WAYS = ["few", "few-flat", "few-shared", "few-halved", "two", "two-shared", "many", "many-shared"]
 SHAPES = [(4, 4, 64, 16), (8, 2, 128, 16), (14, 2, 64, 32), (5, 5, 128, 64), (34, 1, 64, 16), (6, 2, 128, 32)]
 
 
-def stated(way, n_q, n_kv, hd):
-    """Contexts to fill up to with empty ones, queries of the longest, keys of the longest."""
-    full, two = (256 if hd == 64 else 128) * n_kv // n_q, 32 * n_kv // n_q
-    return {"few": (0, 1, 1), "few-shared": (0, 1, 4000), "few-halved": (-(-150 // n_kv), 1, 4000), "two": (-(-640 // n_kv), max(two, 1), 1280),
-            "two-shared": (0, max(two, 1), 1 << 20), "many": (-(-512 // n_kv), full, 1000), "many-shared": (0, full, 1 << 20)}[way]
-
-
-def call_by(way, hc, rng, lens, q_lens, n_q, n_kv, hd, block, **more):
-    n, max_q, max_kv = stated(way, n_q, n_kv, hd)
-    empty = [0] * max(0, n - len(lens))
-    return Call(hc, rng, kh.Cache(rng, lens + empty, n_kv, hd, block), n_q, q_lens + empty, max_q=max_q, max_kv=max_kv, **more)
+def call_by(way, hc, rng, lens, q_lens, n_q, n_kv, hd, block, extra_rows=0, **more):
+    group, tile = n_q // n_kv, 256 if hd == 64 else 128
+    # empty contexts and rows of none, queries of the longest, keys of the longest
+    full, two = tile // group, max(1, 32 // group)
+    empty, padding, max_q, max_kv = {
+        "few": (0, 0, 1, 1), "few-flat": (0, 0, 64, 300), "few-shared": (0, 0, 1, 4000), "few-halved": (-(-150 // n_kv), 0, 1, 4000),
+        "two": (0, 20 * 1024 // n_q, two, 1270), "two-shared": (0, 0, two, 1 << 20),
+        "many": (0, 512 * tile // n_q, full, 1000), "many-shared": (0, 7 * full, full, 1 << 20)}[way]
+    none = [0] * empty
+    return Call(hc, rng, kh.Cache(rng, lens + none, n_kv, hd, block), n_q, q_lens + none, max_q=more.pop("max_q", max_q), max_kv=max_kv,
+                extra_rows=max(padding, extra_rows), **more)
 
 
 @pytest.mark.parametrize("way", WAYS)
@@ -461,7 +461,8 @@ def test_ways_with_positions_in_any_order(hc, way):
 def test_ways_in_a_graph(hc, torch, way):
     rng = np.random.default_rng(25)
     call = call_by(way, hc, rng, [700, 90], [300, 3], 8, 2, 128, 16)
-    want = torch.from_numpy(call.check()).cuda()
+    call.check()
+    want = call.out.clone()
     side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=side):
         call.launch(stream=side.cuda_stream)
@@ -471,4 +472,34 @@ def test_ways_in_a_graph(hc, torch, way):
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()
-        assert torch.equal(call.out.double().view(want.shape), want)
+        assert torch.equal(call.out, want)
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_queries_that_are_not_finite(hc, torch, way):
+    """An infinity or a NaN among a query's channels: that row and head is NaN, all others are what they were."""
+    rng = np.random.default_rng(26)
+    call = call_by(way, hc, rng, [100, 300], [40, 70], 8, 2, 128, 16)
+    call.check()
+    want, want_lse = call.out.clone(), call.lse.clone()
+    width = 8 * 128
+    bad = [(3, 1, 0x7F80), (39, 7, 0x7FC0), (40, 0, 0xFF80), (80, 4, 0xFFC1), (109, 5, 0x7F80)]
+    for row, head, bits in bad:
+        call.d_q.view(torch.int16)[row, head * 128 + 11] = bits - 65536 if bits >= 32768 else bits
+    call.launch()
+    out, lse = call.out[:, :width].reshape(-1, 8, 128), call.lse
+    for row, head, _ in bad:
+        assert torch.isnan(out[row, head]).all() and torch.isnan(lse[row, head])
+        out[row, head], lse[row, head] = want[:, :width].reshape(-1, 8, 128)[row, head], want_lse[row, head]
+    assert torch.equal(call.out, want) and torch.equal(call.lse, want_lse)
+
+
+@pytest.mark.parametrize("n_seq,longest", [(65, 40), (1000, 200), (5000, 64), (4097, 0)])
+def test_many_contexts(hc, n_seq, longest):
+    """Mostly single tokens, places without any, and a prompt among them: every context finds its tiles."""
+    rng = np.random.default_rng([27, n_seq])
+    q_lens = rng.integers(0, 3, n_seq)
+    q_lens[n_seq // 3] = longest
+    q_lens[-1] = 5
+    lens = q_lens + rng.integers(0, 4, n_seq)
+    Call(hc, rng, kh.Cache(rng, lens.tolist(), 1, 64, 16), 4, q_lens.tolist()).check()
