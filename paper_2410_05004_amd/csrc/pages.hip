@@ -9,8 +9,9 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 // blockIdx: (piece of a page, fork, share of the pools); the share behind the last writes the children's table rows.
 // A child's row is its parent's for the full blocks, its own page for a part-filled last one, -1 behind it; of that
 // page the tokens in use are copied.  Parents' rows and children's are different rows, so no order matters.
-// Bound: latency for a few forks (the parent's table entry, then the page), memory for many.  A workgroup looks the page up
-// once and copies the same piece of it, up to 20 KiB, in every so-many-th pool.
+// Bound: latency for a few forks (the parent's table entry, then the page: 8 forks in 32 layers 6 us), memory for many (64 forks of 17 KiB
+// pages in 80 layers 33 us, 5.4 TB/s).  A workgroup looks the page up once and copies the same piece of it, up to 20 KiB, in every
+// so-many-th pool (with a piece of 16 KiB of one pool a workgroup those 64 took 62 us: looking up, and a second piece of 1 KiB).
 constexpr int kForkWords = kForkPiece / 256;   // of a thread
 __global__ __launch_bounds__(256) void fork_kernel(const ForkArgs a) {
   const int f = blockIdx.y, share = blockIdx.z;
@@ -68,13 +69,15 @@ hipError_t launch_fork(const ForkArgs& a, hipStream_t stream) {
 // Live pages (those that a table names) are to be pages 0 .. live - 1: a live page there stays, the others move, in their
 // order, to the free pages among them, in theirs.  One workgroup works the plan out: a bit a page in LDS, set from the
 // tables, then ranks by counting bits: page p's rank among the live is prefix(p); free pages before p are p - prefix(p).
-// Bound: one compute unit's reads of the tables and writes of the map, and latency.
-constexpr int kPlanThreads = 1024;
+// The map and the pairs are written by all of it in one pass over the pages.
+// Bound: one compute unit's reads of the tables and writes of the map, and latency: 500 pages 3.8 us, 2048 4.9, 2^17 57, 2^20 720 (with as
+// many parts as threads 1550: a page's rank is a sum over half a part's words).
+constexpr int kPlanThreads = 1024, kPlanParts = 4096;            // live pages are counted by parts of the bits
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const CompactArgs a) {
   extern __shared__ uint32_t s_bits[];
-  __shared__ int s_before[kPlanThreads + 1], s_wave[kPlanThreads / 64];
+  __shared__ int s_before[kPlanParts], s_wave[kPlanThreads / 64];
   const int tid = threadIdx.x, n = a.num_pages, words = (n + 31) >> 5;
-  const int per = (words + kPlanThreads - 1) / kPlanThreads;     // words of a thread
+  const int per = (words + kPlanParts - 1) / kPlanParts;         // words of a part
   for (int i = tid; i < words; i += kPlanThreads) s_bits[i] = 0;
   __syncthreads();
   bool bad = false;
@@ -93,10 +96,15 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const Compac
   }
   if (bad) atomicOr(a.err, HC_DEV_BAD_PAGE);
   __syncthreads();
-  int mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int w = tid * per + i;
-    if (w < words) mine += __popc(s_bits[w]);
+  constexpr int kMine = kPlanParts / kPlanThreads;
+  int part[kMine], mine = 0;
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) {
+    part[u] = mine;
+    for (int i = 0; i < per; ++i) {
+      const int w = (tid * kMine + u) * per + i;
+      if (w < words) mine += __popc(s_bits[w]);
+    }
   }
   int sum = mine;                                                // inclusive over the wave, then over the waves
 #pragma unroll
@@ -106,18 +114,22 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const Compac
   }
   if ((tid & 63) == 63) s_wave[tid >> 6] = sum;
   __syncthreads();
-  for (int i = 0; i < (tid >> 6); ++i) sum += s_wave[i];
-  s_before[tid] = sum - mine;
-  if (tid == kPlanThreads - 1) s_before[kPlanThreads] = sum;
+  int live = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanThreads / 64; ++i) {
+    if (i < (tid >> 6)) sum += s_wave[i];
+    live += s_wave[i];
+  }
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) s_before[tid * kMine + u] = sum - mine + part[u];
   __syncthreads();
-  const int live = s_before[kPlanThreads];
   auto prefix = [&](int p) __attribute__((always_inline)) {      // live pages before p
     const int w = p >> 5, t = w / per;
     int c = s_before[t];
     for (int i = t * per; i < w; ++i) c += __popc(s_bits[i]);
     return c + (p & 31 ? __popc(s_bits[w] & ((1u << (p & 31)) - 1)) : 0);
   };
-  const int stay = prefix(live), moves = live - stay;
+  const int stay = live < n ? prefix(live) : n, moves = live - stay;
   int32_t* map = a.plan + 2;
   int32_t* pairs = map + n;
   if (tid == 0) { a.plan[0] = live; a.plan[1] = moves; }
@@ -135,7 +147,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const Compac
 }
 
 // Pages to their new places, in every pool, 16 KiB a step, and the tables through the map.  The launch does not know
-// how many there are.  Bound: memory.
+// how many there are.  Bound: memory: 32 layers' bf16 pages of 64 KiB, 454 moves, 364 us, 5.2 TB/s read and written (a large copy: 4.9).
 __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a) {
   const int32_t* map = a.plan + 2;
   const int32_t* pairs = map + a.num_pages;
