@@ -28,8 +28,9 @@ __device__ __forceinline__ int context_of(const int32_t* cu, int n_seq, int t, i
 //   scale = smallest 2^e with top <= 7 * 2^e: with top = 1.m * 2^E, e = E - 2 if 1.m <= 1.75, else E - 1
 // (then no value is further from its code than half a step); codes by the conversion instruction, to nearest, ties to even.
 // Consecutive tokens make whole sub-blocks, so a workgroup's stores fill the lines that they touch.
-// Bound: memory (2 + 17 / 32 bytes a value): 32768 tokens of 8 heads of 128, 170 MB, 42 us in, 44 out (4.0 TB/s; a large copy: 4.9), from bf16
-// pages 37; 2501 tokens of 40 heads 18 and 19; 64 tokens of 8 heads 3, latency.
+// Rows go past the caches, codes do not: they are what is read next, and fill lines by the store of several waves.
+// Bound: memory (2 + 17 / 32 bytes a value): 32768 tokens of 8 heads of 128, 170 MB, 38 us in, 31 out (4.5 and 5.5 TB/s; a large copy: 4.9; rows
+// through the caches 44 and 46), 2501 tokens of 40 heads, 65 MB, 17 and 12 (18 and 19); 64 tokens of 8 heads 3, latency.
 template <Kv4Move MOVE>
 __global__ __launch_bounds__(256) void kv4_rows_kernel(const Kv4RowsArgs a) {
   const int t = blockIdx.x * 16 + (threadIdx.x >> 4), c = threadIdx.x & 15;
@@ -81,14 +82,14 @@ __global__ __launch_bounds__(256) void kv4_rows_kernel(const Kv4RowsArgs a) {
       out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
       out[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
       out[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
-      *reinterpret_cast<u32x4*>(a.rows + (size_t)t * (2 * a.d_kv) + col) = out;
+      __builtin_nontemporal_store(out, reinterpret_cast<u32x4*>(a.rows + (size_t)t * (2 * a.d_kv) + col));
     } else {
       u32x4 x = {0, 0, 0, 0};
       if (ok) {
         const uint16_t* src = MOVE == Kv4Move::kRowsToCodes
             ? a.rows + (size_t)t * (2 * a.d_kv) + col
             : a.src_pool + ((((size_t)src_page * 2 + part) << a.block_shift) + slot) * a.d_kv + ch_all;
-        x = *reinterpret_cast<const u32x4*>(src);
+        x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src));
       }
       uint32_t top = 0;
 #pragma unroll
