@@ -503,3 +503,12 @@ def test_many_contexts(hc, n_seq, longest):
     q_lens[-1] = 5
     lens = q_lens + rng.integers(0, 4, n_seq)
     Call(hc, rng, kh.Cache(rng, lens.tolist(), 1, 64, 16), 4, q_lens.tolist()).check()
+
+
+def test_more_contexts_than_one_dimension_has_places(hc):
+    """A place a context, up to four queries: 40000 of them, the last ones beyond 32768."""
+    rng = np.random.default_rng(28)
+    q_lens = rng.integers(0, 5, 40000) * (rng.random(40000) < 0.2)
+    q_lens[[0, 32767, 32768, 39999]] = [1, 2, 3, 4]
+    lens = q_lens + rng.integers(0, 2, 40000) * (q_lens > 0)
+    Call(hc, rng, kh.Cache(rng, lens.tolist(), 1, 64, 16), 4, q_lens.tolist()).check()

@@ -274,3 +274,32 @@ def test_a_cache_in_use(hc, torch):
     again = attend(child, q[1:], [n + 1], both[1:])
     assert torch.equal(again[0], out[1])
     ctx.destroy()
+
+
+def test_compact_many_pages_in_a_graph(hc, torch):
+    """A plan whose bits need more LDS than a launch has by itself, captured; the replays find less and less to do."""
+    num_pages, live = 300000, 1000
+    rng = np.random.default_rng(38)
+    pool = torch.zeros((num_pages, 1, 1, 17 * 64), dtype=torch.uint8, device="cuda")
+    ctx = kh.context(hc, 1, 1, 64, 16)
+    ctx.set_kv4_pool(0, pool, num_pages)
+    d_tab, plan = torch.zeros((10, 100), dtype=torch.int32, device="cuda"), torch.zeros((2 + 2 * num_pages,), dtype=torch.int32, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        ctx.compact_pages(hc.HC_POOL_KV4, d_tab, d_tab, 10, 100, plan, side.cuda_stream)
+    for i in range(3):
+        named = rng.permutation(num_pages)[:live].astype(np.int32)
+        marks = torch.from_numpy(rng.integers(0, 256, (live, 17 * 64)).astype(np.uint8)).cuda()
+        pool.view(num_pages, -1)[torch.from_numpy(named).cuda().long()] = marks
+        d_tab.copy_(gh.to_dev_i32(named.reshape(10, 100)))
+        for again in range(2):
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert ctx.poll_device_error(gh.stream_handle()) == 0
+            assert plan[:2].tolist() == [live, 0 if again else int((named >= live).sum())]
+            now = d_tab.cpu().numpy().reshape(-1)
+            assert sorted(now.tolist()) == list(range(live)) and np.array_equal(now[named < live], named[named < live])
+            assert torch.equal(pool.view(num_pages, -1)[d_tab.view(-1).long()], marks)
+    ctx.destroy()
