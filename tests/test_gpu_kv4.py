@@ -512,3 +512,22 @@ def test_more_contexts_than_one_dimension_has_places(hc):
     q_lens[[0, 32767, 32768, 39999]] = [1, 2, 3, 4]
     lens = q_lens + rng.integers(0, 2, 40000) * (q_lens > 0)
     Call(hc, rng, kh.Cache(rng, lens.tolist(), 1, 64, 16), 4, q_lens.tolist()).check()
+
+
+@pytest.mark.parametrize("way", ["few", "few-flat", "few-shared", "few-halved", "many", "many-shared"])
+@pytest.mark.parametrize("n_q,n_kv", [(4, 2), (3, 3), (20, 1)])
+def test_ways_of_256_channels(hc, way, n_q, n_kv):
+    """Heads that take the same rows to a workgroup whatever their number: whole, with shares joined by four groups or by sixteen."""
+    rng = np.random.default_rng([29, n_q])
+    lens, q_lens = [50, 7, 130, 300, 20, 1], [50, 9, 1, 77, 0, 1]
+    call = call_by(way, hc, rng, lens, q_lens, n_q, n_kv, 256, 16, pad=8, q_extra=16, extra_rows=3)
+    call.check()
+    cache = call.cache
+    for part, s, head, key, group in ((1, 0, n_kv - 1, 30, 7), (0, 3, 0, 295, 3), (1, 3, 0, 261, 0)):
+        page, slot = cache.tables[s, key // 16], key % 16
+        cache.pool[page, head, 0][kv4.places(part, head, slot, 256)[2][group]] = 255
+    cache.tables[2, 3] = -1
+    call.pool.copy_(kh.dev_u8(cache.pool))
+    call.d["tab"].copy_(gh.to_dev_i32(cache.tables))
+    out = call.check(flags=hc.HC_DEV_BAD_PAGE)
+    assert np.isnan(out).any() and not np.isnan(out).all()
