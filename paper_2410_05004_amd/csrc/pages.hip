@@ -146,8 +146,10 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const Compac
   for (int i = tid; i < moves; i += kPlanThreads) map[pairs[2 * i]] = pairs[2 * i + 1];
 }
 
-// Pages to their new places, in every pool, 16 KiB a step, and the tables through the map.  The launch does not know
-// how many there are.  Bound: memory: 32 layers' bf16 pages of 64 KiB, 454 moves, 364 us, 5.2 TB/s read and written (a large copy: 4.9).
+// Pages to their new places, in every pool, in steps of up to 20 KiB, equal ones of a page, and the tables through the map.  The launch does
+// not know how many there are.  Bound: memory: 32 layers' bf16 pages of 64 KiB, 454 moves, 356 us, 5.3 TB/s read and written (a large copy: 4.9);
+// 8 layers' 4-bit pages of 17 KiB, 34 MB, 6 to 7 us (in steps of 16 KiB, every other one of 1 KiB, 9 to 10).
+constexpr int kMovePiece = 5 * 256;        // words of a step at most
 __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a) {
   const int32_t* map = a.plan + 2;
   const int32_t* pairs = map + a.num_pages;
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a) 
   for (int kind = 0; kind < 2; ++kind) {
     const int first = kind ? a.pools.first4 : 0, n_pools = (kind ? a.pools.n_pools : a.pools.first4) - first;
     if (n_pools <= 0) continue;
-    const int words = a.pools.shape[kind].words, pieces = (words + 1023) >> 10;
+    const int words = a.pools.shape[kind].words, pieces = (words + kMovePiece - 1) / kMovePiece, length = (words + pieces - 1) / pieces;
     const int64_t items = (int64_t)moves * n_pools * pieces;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
       const int64_t pair = it / pieces;
@@ -168,14 +170,14 @@ __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a) 
       u32x4* base = static_cast<u32x4*>(a.pools.pool[first + pool]);
       const u32x4* from = base + (size_t)pairs[2 * move] * words;
       u32x4* to = base + (size_t)pairs[2 * move + 1] * words;
-      const int i0 = piece * 1024 + threadIdx.x;
-      u32x4 v[4];
+      const int i0 = piece * length + threadIdx.x, end = piece * length + length < words ? piece * length + length : words;
+      u32x4 v[kMovePiece / 256];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i0 + u * 256 < words) v[u] = __builtin_nontemporal_load(from + i0 + u * 256);
+      for (int u = 0; u < kMovePiece / 256; ++u)
+        if (i0 + u * 256 < end) v[u] = __builtin_nontemporal_load(from + i0 + u * 256);
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i0 + u * 256 < words) __builtin_nontemporal_store(v[u], to + i0 + u * 256);
+      for (int u = 0; u < kMovePiece / 256; ++u)
+        if (i0 + u * 256 < end) __builtin_nontemporal_store(v[u], to + i0 + u * 256);
     }
   }
 }
