@@ -7,7 +7,7 @@ namespace hc {
 // A workgroup takes 128 * NB rows, 32 * NB to a wave, and a share of the keys in tiles of 64.  Each wave decodes a quarter of
 // a tile into LDS, as the operands of v_mfma_f32_32x32x16 (1 KiB a fragment, 16 bytes a lane in lane order), while all of
 // them work on the tile before; the bytes of the tile behind are on their way to registers meanwhile.
-// Bound: issue: 8 contexts of up to 2048 queries on 4096 keys, 40 heads of 128, 454 GFLOP, 507 to 540 us (0.84 to 0.90 PFLOP/s; a large product of
+// Bound: issue: 8 contexts of up to 2048 queries on 4096 keys, 40 heads of 128, 454 GFLOP, 502 to 525 us (0.86 to 0.90 PFLOP/s; a large product of
 // the library's reaches 1.21), matrix instructions 43 % of the cycles and vector ones 49: of a wave's 32 rows and 64 keys, 32 matrix
 // instructions of 32 cycles, the softmax's 2048 exponentials and its maxima and sums beside them, and a quarter of the tile's decoding.
 // 32 x 32 products take half the issue slots of 16 x 16 ones; a second workgroup on the compute unit fills the barriers.
@@ -140,15 +140,32 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
       f32x16 x[NB];
       float most[NB];
     };
-    auto products = [&](Scores& s, int buf, int pair) __attribute__((always_inline)) {       // S^T = K Q^T
+    // Operands of 32 keys, read together: the compiler by itself reads each into the registers of the one before, right before its
+    // use, and waits (8 contexts of up to 2048 queries on 4096 keys, 40 heads of 128: 884 us, so 902; one on 16000 keys 737 and 785).
+    struct KeyParts {
+      bf16x8 k[kSteps];
+    };
+    struct ValueParts {
+      bf16x8 v[2][kBlocks];
+    };
+    auto read_keys = [&](KeyParts& f, int buf, int pair) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) f.k[j] = __builtin_bit_cast(bf16x8, s_k[buf][pair][j][lane]);
+      __builtin_amdgcn_sched_barrier(6);             // vector and scalar instructions may pass, the products and the next reads may not
+    };
+    auto read_values = [&](ValueParts& f, int buf, int pair) __attribute__((always_inline)) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int c = 0; c < kBlocks; ++c) f.v[m][c] = __builtin_bit_cast(bf16x8, s_v[buf][pair][m][c][lane]);
+    };
+    auto products = [&](Scores& s, const KeyParts& f) __attribute__((always_inline)) {       // S^T = K Q^T
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) s.x[nb] = f32x16{};
 #pragma unroll
-      for (int j = 0; j < kSteps; ++j) {
-        const bf16x8 k = __builtin_bit_cast(bf16x8, s_k[buf][pair][j][lane]);
+      for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s.x[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[nb][j], s.x[nb], 0, 0, 0);
-      }
+        for (int nb = 0; nb < NB; ++nb) s.x[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.k[j], q[nb][j], s.x[nb], 0, 0, 0);
     };
     auto most_of = [&](Scores& s) __attribute__((always_inline)) {
 #pragma unroll
@@ -176,15 +193,13 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
           w[nb][v >> 3][v & 7] = (__bf16)e;
         }
     };
-    auto add_values = [&](const bf16x8 (&w)[NB][2], int buf, int pair) __attribute__((always_inline)) {   // O^T += V^T W^T
+    auto add_values = [&](const bf16x8 (&w)[NB][2], const ValueParts& f) __attribute__((always_inline)) {   // O^T += V^T W^T
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int c = 0; c < kBlocks; ++c) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, s_v[buf][pair][m][c][lane]);
+        for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[nb][m], o[nb][c], 0, 0, 0);
-        }
+          for (int nb = 0; nb < NB; ++nb) o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v[m][c], w[nb][m], o[nb][c], 0, 0, 0);
     };
     // What new scores ask for now and then: masks, NaN among the values, a higher top.
     auto settle = [&](Scores& s, int tile, int buf, int pair, int gone) __attribute__((always_inline)) {
@@ -264,7 +279,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
       gone_k = missing(from_tile + 2);
       rk.load(at, l16, q4);
       __syncthreads();
-      products(s0, 0, 0);
+      KeyParts k0;
+      read_keys(k0, 0, 0);
+      products(s0, k0);
       above_top(s0);
       for (int tile = from_tile; tile < to_tile; ++tile) {
         const int buf = (tile - from_tile) & 1;
@@ -276,9 +293,13 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
           Scores& next = pair & 1 ? s0 : s1;
           if (last) __syncthreads();                 // the next tile's values are there, and this one's keys are not needed any more
           settle(now, tile, buf, pair, gone);
-          products(next, last ? buf ^ 1 : buf, last ? 0 : pair + 1);
+          KeyParts k;
+          ValueParts v;
+          read_keys(k, last ? buf ^ 1 : buf, last ? 0 : pair + 1);
+          products(next, k);
+          read_values(v, buf, pair);
           weights(w, now);
-          add_values(w, buf, pair);
+          add_values(w, v);
           above_top(next);
           if (pair == 0) {
             decode_values(buf ^ 1);
