@@ -358,7 +358,11 @@ hc_status hc_dequantize_kv(hc_ctx* ctx, int32_t layer, void* d_rows, const int32
  * were.  Keys on pages that are none of the pool's count as unseen and raise HC_DEV_BAD_PAGE; key counts below 0, beyond
  * the table or beyond 2^30 are clamped and raise HC_DEV_BAD_POSITION.  What unseen slots hold does not matter.
  * h_max_q and h_max_kv should be the most queries and keys of a context: the launch is laid out by them, results do not
- * depend on them but for the order of sums.
+ * depend on them but for the order of sums and the rounding of weights.
+ * Keys and values enter as they are stored; scores, weights and sums are fp32.  For the product with the values a weight goes into the
+ * matrix instructions as two numbers of bf16, 2^-17 of it off at most, where contexts have up to 8 rows (h_max_q * n_q_heads /
+ * n_kv_heads <= 8, and the context's queries too: single tokens mostly), so that outputs are rounded once; in all other calls as one, 2^-8 off at
+ * most, each by itself (relative to their norm outputs are then off by some 0.0023, once rounded ones by 0.0017).  d_lse has the fp32 sums.
  *   d_workspace    16-byte aligned, workspace_bytes >= hc_attend_kv4_workspace of the same sizes (HC_EINVAL); used by this launch
  *                  alone until it is done: calls that may run at the same time, and graphs that may, need one each.  NULL when the
  *                  size is 0.

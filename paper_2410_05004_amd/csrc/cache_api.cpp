@@ -348,7 +348,7 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
   a.flat = plan.flat;
   a.n_slots = plan.n_slots;
   a.n_split = plan.n_split;
-  HC_HIP(launch_attend(a, d.head_dim, plan.row_blocks, static_cast<hipStream_t>(stream)));
+  HC_HIP(launch_attend(a, d.head_dim, plan, static_cast<hipStream_t>(stream)));
   return HC_OK;
 }
 

@@ -67,8 +67,10 @@ struct AttendPlan {
   // Places for workgroups along the rows, of a KV head and share of the keys: one a context, which goes through all of its tiles of rows
   // (one, if the sizes are right); or, flat, one a tile: context s has those from cu[s] * group / size + s on, up to one too many.
   int32_t flat, n_slots, n_split;
+  bool paired;                             // contexts have up to kPairedRows rows, whose weights are kept in two parts of bf16
   int64_t workspace;                       // bytes
 };
+constexpr int kPairedRows = 8;             // half of a block
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv);
 bool attend_head_dim(int head_dim);
 int attend_rows_blocks(int head_dim);      // row blocks of a workgroup of launch_attend_rows, which takes heads of 64 and 128
@@ -77,6 +79,6 @@ inline dim3 attend_grid(const AttendArgs& a) {      // places over two dimension
   return dim3(a.n_split * a.n_kv, y, (a.n_slots + y - 1) / y);
 }
 void launch_attend_rows(const AttendArgs& a, int head_dim, hipStream_t stream);
-hipError_t launch_attend(const AttendArgs& a, int head_dim, int row_blocks, hipStream_t stream);
+hipError_t launch_attend(const AttendArgs& a, int head_dim, const AttendPlan& plan, hipStream_t stream);
 
 }  // namespace hc

@@ -11,8 +11,8 @@
 // has been seen to put a copy that it needs for all lanes into a branch that some had not taken (sums of the second 16 rows were
 // wrong at 256 channels, the registers in question traced in the generated code).  What concerns some lanes is selected, and what
 // several would store alike they all do.
-// Decoded keys and values are exact in bf16; W is rounded to bf16 (2^-9 relative, without a bias, which averages out over
-// the keys), sums and statistics are fp32.
+// Decoded keys and values are exact in bf16; W is rounded to bf16 (2^-8 relative at most, without a bias, which averages out over
+// the keys), in two parts where rows are few (see PAIRED); sums and statistics are fp32.
 #include <algorithm>
 
 #include "kv4_device.h"
@@ -23,12 +23,18 @@ namespace hc {
 // NB blocks of 16 rows and a share of the keys; its waves take every so-many-th step of 32 keys, for all the rows.
 // The next step's bytes are fetched into the registers as soon as this step's are decoded: keys before the softmax, values
 // behind the second product.
-// Bound, single tokens: memory, where there are keys enough (32 heads over 8 of 128: 64 contexts of up to 8192 keys, 374 MB, 80 us, 4.7 TB/s; 64
-// heads over 8, one context of 131072 keys, 143 MB, 25.5 us, 5.6 TB/s; a large sum reads 5.6); else latency: one context of 1037 keys 10.7 us,
-// of which 5.8 for the launch, the lengths, the table and the first keys, and 0.5 for each step of the four waves.  Some 16 rows: 4 waves
+// Bound, single tokens: memory, where there are keys enough (32 heads over 8 of 128: 64 contexts of up to 8192 keys, 374 MB, 82 us, 4.6 TB/s; 64
+// heads over 8, one context of 131072 keys, 143 MB, 26.5 us, 5.4 TB/s; a large sum reads 5.6); else latency: one context of 1037 keys 11.1 us,
+// of which 5.8 for the launch, the lengths, the table and the first keys, and 0.5 to 0.6 for each step of the four waves.  Some 16 rows: 4 waves
 // are better than 8 or 16 (64 contexts of up to 4000 keys 38, 41, 58 us; one of 1000 9.9, 9.9, 15).
+//
+// Weights are rounded to bf16 for the second product.  Where a call's contexts have up to 8 rows, half of a block's 16 columns would compute
+// a row twice: PAIRED, columns 8 .. 15 take the same rows with what the rounding took from the weights, to bf16 again, and the two halves
+// are added at the end: 2^-17 at most is lost then (in norm outputs are off by 0.0017 as if rounded once, instead of 0.0023).  Costs 2.5
+// instructions a weight: one context of 1037 keys 10.8 us without, 11.1 with, the 64 contexts 80.4 and 82.4.  A second product over the same
+// columns costs more (11.6 and 84.6; one context's 1024 queries on 4000 keys 95 us instead of 75), so other calls have the rounded weights alone.
 constexpr int kFewWaves = 4;
-template <int HD, int NB>
+template <int HD, int NB, bool PAIRED>
 __global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256 ? 2 : 1) void attend_kernel(const AttendArgs a) {
   constexpr int kSteps = HD / 32;         // matrix ops along the channels
   constexpr int kSlices = HD / 16;        // blocks of 16 channels of the result
@@ -38,6 +44,10 @@ __global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256
   const int split = blockIdx.x % a.n_split, kvh = blockIdx.x / a.n_split;
   const Task task(a, NB * 16);
   const int seq = task.seq, q0 = task.q0, n_rows = task.n_rows;
+  const bool paired = PAIRED && n_rows <= kPairedRows;
+  // of a pair of rounded weights, what a lane's column takes from the weights themselves: the first or second, or nothing
+  const bool rest = paired && l16 >= kPairedRows;
+  const uint32_t first_of = rest ? 0x01000c0cu : 0x0c0c0c0cu, second_of = rest ? 0x03020c0cu : 0x0c0c0c0cu;
   const int64_t room = (int64_t)a.max_blocks << a.block_shift, most = room < kMaxKeys ? room : kMaxKeys;
   int keys = uniform(a.kv_lens)[seq];
   if (keys > most || keys < 0) {
@@ -52,11 +62,11 @@ __global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256
     // ---- this workgroup's share of the keys, in steps of 32: of all that there are, or, if there is a window, of those that any row
     // sees.  Without one nothing waits for the positions: the table's entries and the rows are on their way together.
     auto query_of = [&](int nb) __attribute__((always_inline)) {
-      const int r = (tile * NB + nb) * 16 + l16;
+      const int r = (tile * NB + nb) * 16 + (paired ? l16 & 7 : l16);
       return (r < n_rows ? r : n_rows - 1) / a.group;
     };
     auto head_of = [&](int nb, int query) __attribute__((always_inline)) {
-      const int r = (tile * NB + nb) * 16 + l16;
+      const int r = (tile * NB + nb) * 16 + (paired ? l16 & 7 : l16);
       return kvh * a.group + (r < n_rows ? r : n_rows - 1) - query * a.group;
     };
     const int lane_key = (lane >> 1) * 32 * kFewWaves + (lane & 1) * 16;        // run i of a round: half i % 2 of this wave's step i / 2
@@ -202,10 +212,19 @@ __global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][h][v], a.scale_log2, -used[nb]));
-            sum[nb] += e;
-            w[nb][4 * h + v] = (__bf16)e;
+          for (int v = 0; v < 4; v += 2) {
+            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][h][v], a.scale_log2, -used[nb]));
+            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][h][v + 1], a.scale_log2, -used[nb]));
+            sum[nb] += e0;
+            sum[nb] += e1;
+            bf16x2 p = __builtin_convertvector(f32x2{e0, e1}, bf16x2);
+            if constexpr (PAIRED) {
+              const uint32_t bits = __builtin_bit_cast(uint32_t, p);
+              p = __builtin_convertvector(f32x2{e0 - __uint_as_float(__builtin_amdgcn_perm(0, bits, first_of)),
+                                                e1 - __uint_as_float(__builtin_amdgcn_perm(0, bits, second_of))}, bf16x2);
+            }
+            w[nb][4 * h + v] = p[0];
+            w[nb][4 * h + v + 1] = p[1];
           }
       }
       // ---- O^T += V^T W^T: byte i of a key's word holds slices 2 i and 2 i + 1
@@ -275,6 +294,13 @@ __global__ __launch_bounds__(64 * kFewWaves, NB * HD <= 128 ? 3 : NB * HD <= 256
       }
     }
     if (wave == 0) {
+      if (paired) {
+#pragma unroll
+        for (int b = 0; b < kSlices; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            o[0][b][v] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o[0][b][v]), 0x128, 0xf, 0xf, false));
+      }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if ((tile * NB + nb) * 16 >= n_rows) continue;       // places behind the last row have computed that row too and store the same
@@ -414,6 +440,7 @@ AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, 
   const bool filled = 4 * rows >= 3 * ((rows + many - 1) / many) * many && all_rows >= (even ? 3 * many / 4 : 8 * many) * n_seq;
   const bool some = rows > 16 && (even || all_rows >= 64 * (int64_t)n_seq);
   p.row_blocks = row_blocks(head_dim, tiles_of(16), max_kv, tiles_of(many), some, filled);
+  p.paired = p.row_blocks == 1 && rows <= kPairedRows;
   const int64_t size = 16 * p.row_blocks;
   // a place a tile: contexts of very different sizes then leave next to none empty (8192 queries and 255 times one: 774 us; with places
   // for the longest in every context 1760)
@@ -425,14 +452,15 @@ AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, 
 }
 
 template <int HD>
-static void launch_hd(const AttendArgs& a, int row_blocks, hipStream_t stream) {
+static void launch_hd(const AttendArgs& a, const AttendPlan& plan, hipStream_t stream) {
   const dim3 grid = attend_grid(a);
-  if (row_blocks > 2) {
+  if (plan.row_blocks > 2) {
     launch_attend_rows(a, HD, stream);
-  } else if (row_blocks == 1) {
-    hipLaunchKernelGGL((attend_kernel<HD, 1>), grid, dim3(64 * kFewWaves), 0, stream, a);
+  } else if (plan.row_blocks == 1) {
+    if (plan.paired) hipLaunchKernelGGL((attend_kernel<HD, 1, true>), grid, dim3(64 * kFewWaves), 0, stream, a);
+    else             hipLaunchKernelGGL((attend_kernel<HD, 1, false>), grid, dim3(64 * kFewWaves), 0, stream, a);
   } else if constexpr (HD <= 128) {
-    hipLaunchKernelGGL((attend_kernel<HD, 2>), grid, dim3(64 * kFewWaves), 0, stream, a);
+    hipLaunchKernelGGL((attend_kernel<HD, 2, false>), grid, dim3(64 * kFewWaves), 0, stream, a);
   }
   if (a.n_split > 1) {
     const int64_t n_row = (int64_t)a.total_q * a.n_q;
@@ -441,12 +469,12 @@ static void launch_hd(const AttendArgs& a, int row_blocks, hipStream_t stream) {
   }
 }
 
-hipError_t launch_attend(const AttendArgs& a, int head_dim, int row_blocks, hipStream_t stream) {
+hipError_t launch_attend(const AttendArgs& a, int head_dim, const AttendPlan& plan, hipStream_t stream) {
   if (a.total_q <= 0 || a.n_seq <= 0) return hipSuccess;
   switch (head_dim) {
-    case 64: launch_hd<64>(a, row_blocks, stream); break;
-    case 128: launch_hd<128>(a, row_blocks, stream); break;
-    case 256: launch_hd<256>(a, row_blocks, stream); break;
+    case 64: launch_hd<64>(a, plan, stream); break;
+    case 128: launch_hd<128>(a, plan, stream); break;
+    case 256: launch_hd<256>(a, plan, stream); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
