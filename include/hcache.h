@@ -379,7 +379,7 @@ hc_status hc_attend_kv4_workspace(const hc_model_desc* desc, int32_t n_seq, int3
 /* ---- pages as a whole ------------------------------------------------------------------------
  * Block tables are int32 [n_rows][max_blocks] on the device, shared by all layers; `pools` names the pools that go by
  * them: HC_POOL_KV (bf16), HC_POOL_KV4 (4 bits) or both.  Every layer needs each of them (HC_ESTATE), all of the same
- * number of pages (HC_EINVAL). */
+ * number of pages, and a page of either below 2 GiB (HC_EINVAL). */
 enum { HC_POOL_KV = 1, HC_POOL_KV4 = 2 };
 
 /* Fork contexts: row h_to_rows[i] of the tables becomes a context of the first h_n_tok[i] tokens of row h_from_rows[i].  Full blocks

@@ -106,7 +106,9 @@ hc_status page_pools(const hc_ctx* ctx, int32_t pools, std::vector<void*>& list,
       list.push_back(p);
     }
   }
-  const int kv_half = d.block_size * ctx->d_kv / 8;          // 16-byte words; d_kv is a multiple of 64
+  const int64_t half_words = (int64_t)d.block_size * ctx->d_kv / 8;    // 16-byte words; d_kv is a multiple of 64
+  if ((pools & HC_POOL_KV) && 2 * half_words * 16 > INT_MAX) return fail(HC_EINVAL, "a page of the bf16 cache must stay below 2 GiB");
+  const int kv_half = pools & HC_POOL_KV ? (int)half_words : 0;
   shape[0] = PageShape{2 * kv_half, 2, kv_half, ctx->d_kv / 8, 0};
   if (pools & HC_POOL_KV4) {
     const int sub = sub_bytes(d.head_dim) / 16, head = d.block_size / kSubTokens * sub;

@@ -10,8 +10,8 @@ constexpr int kForkPiece = 5 * 256;       // 16-byte words of a page that a work
 constexpr int kPoolsPerLaunch = 128;      // pools (a layer's bf16 or 4-bit one) per launch
 constexpr int kMaxCompactPages = 1 << 20; // one bit each in a compute unit's LDS
 
-// A page of a pool: what a fork copies of it are `runs` runs, `stride` bytes apart, of `unit` bytes for every
-// `unit_tokens` tokens begun (bf16: K and V; 4 bits: the KV heads).  All in 16-byte words.
+// A page of a pool, `words` 16-byte words: what a fork copies of it are `runs` runs, `stride` words apart, of `unit` words for every
+// 2^unit_shift tokens begun (bf16: K and V; 4 bits: the KV heads).
 struct PageShape {
   int32_t words, runs, stride, unit, unit_shift;
 };
