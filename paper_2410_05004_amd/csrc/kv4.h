@@ -16,7 +16,6 @@ namespace hc {
 // token l16, channels q4 * hd / 4 .. (hd / 4 of them, in steps of 8); as the rows of V^T the channels of slice l16 and
 // tokens 4 * q4 .. + 3.  Either is hd / 8 consecutive bytes, and the lanes' bytes lie side by side.
 constexpr int kSubTokens = 16;
-constexpr int kScaleGroup = 32;
 __host__ __device__ constexpr int sub_bytes(int hd) { return 17 * hd; }
 __host__ __device__ constexpr int v_codes_at(int hd) { return 8 * hd; }
 __host__ __device__ constexpr int k_scales_at(int hd) { return 16 * hd; }
