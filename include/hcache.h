@@ -372,9 +372,13 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
                         int32_t h_max_kv, const int32_t* d_block_tables, int32_t max_blocks, float scale, int32_t window,
                         void* d_out, int64_t out_stride, float* d_lse, void* d_workspace, int64_t workspace_bytes,
                         void* stream);
-/* Bytes of workspace of such a call (0 where it needs none); host only. */
+/* Bytes of workspace of such a call (0 where it needs none); host only.  A smaller call may need more: few contexts share their
+ * keys among more workgroups than many do. */
 hc_status hc_attend_kv4_workspace(const hc_model_desc* desc, int32_t n_seq, int32_t h_total_q, int32_t h_max_q,
                                   int32_t h_max_kv, int64_t* out_bytes);
+/* Bytes that are enough for every call of up to h_total_q queries and h_max_kv keys a context, whatever its other sizes (for a
+ * workspace that a program keeps): some 34 MB at most; host only. */
+hc_status hc_attend_kv4_workspace_bound(const hc_model_desc* desc, int32_t h_total_q, int32_t h_max_kv, int64_t* out_bytes);
 
 /* ---- pages as a whole ------------------------------------------------------------------------
  * Block tables are int32 [n_rows][max_blocks] on the device, shared by all layers; `pools` names the pools that go by

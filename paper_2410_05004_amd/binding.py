@@ -84,6 +84,7 @@ def _load():
         "hc_attend_kv4": (i32, [vp, i32, vp, i64, vp, i32, vp, vp, i32, i32, i32, vp, i32, C.c_float, i32,
                                 vp, i64, vp, vp, i64, vp]),
         "hc_attend_kv4_workspace": (i32, [p(ModelDesc), i32, i32, i32, i32, p(i64)]),
+        "hc_attend_kv4_workspace_bound": (i32, [p(ModelDesc), i32, i32, p(i64)]),
         "hc_fork_pages": (i32, [vp, i32, vp, i32, i32, vp, vp, vp, vp, i32, vp]),
         "hc_compact_pages": (i32, [vp, i32, vp, vp, i32, i32, vp, vp]),
         "hc_restore_contexts": (i32, [vp, vp, i32, vp, vp, vp, i32, vp, vp]),
@@ -125,7 +126,7 @@ EXPORTED = ("hc_last_error hc_version hc_validate_desc hc_create hc_destroy hc_s
             "hc_saver_fence hc_restore_kv_layers hc_restore_contexts hc_timing_end_stats "
             "hc_restore_context_static hc_static_stage_bytes hc_poison_staging hc_diag_mfma_duty hc_diag_tile_map hc_set_split hc_diag_split_plan hc_diag_route hc_diag_tile "
             "hc_kv4_page_bytes hc_set_kv4_pool hc_quantize_kv hc_quantize_kv_pages hc_dequantize_kv hc_attend_kv4 "
-            "hc_attend_kv4_workspace hc_fork_pages hc_compact_pages").split()
+            "hc_attend_kv4_workspace hc_attend_kv4_workspace_bound hc_fork_pages hc_compact_pages").split()
 
 
 def _check(status):
@@ -209,6 +210,13 @@ def attend_kv4_workspace(desc, n_seq, total_q, max_q, max_kv):
     """Bytes of workspace that Context.attend_kv4 needs for these sizes."""
     out = C.c_int64(0)
     _check(lib.hc_attend_kv4_workspace(C.byref(desc), n_seq, total_q, max_q, max_kv, C.byref(out)))
+    return out.value
+
+
+def attend_kv4_workspace_bound(desc, total_q, max_kv):
+    """Bytes of workspace that are enough for every call of Context.attend_kv4 of up to these sizes."""
+    out = C.c_int64(0)
+    _check(lib.hc_attend_kv4_workspace_bound(C.byref(desc), total_q, max_kv, C.byref(out)))
     return out.value
 
 

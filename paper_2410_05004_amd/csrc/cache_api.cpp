@@ -291,6 +291,17 @@ hc_status hc_attend_kv4_workspace(const hc_model_desc* desc, int32_t n_seq, int3
   return HC_OK;
 }
 
+hc_status hc_attend_kv4_workspace_bound(const hc_model_desc* desc, int32_t h_total_q, int32_t h_max_kv, int64_t* out_bytes) {
+  clear_error();
+  if (!out_bytes) return fail(HC_EINVAL, "null output pointer");
+  hc_status s = check_desc(desc);
+  if (s == HC_OK) s = check_kv4(*desc);
+  if (s != HC_OK) return s;
+  if (h_total_q < 0 || h_max_kv < 0) return fail(HC_EINVAL, "negative size");
+  *out_bytes = attend_workspace_bound(desc->n_q_heads, desc->n_kv_heads, desc->head_dim, h_total_q, h_max_kv);
+  return HC_OK;
+}
+
 hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_stride, const int32_t* d_positions,
                         int32_t h_total_q, const int32_t* d_cu_q, const int32_t* d_kv_lens, int32_t n_seq, int32_t h_max_q,
                         int32_t h_max_kv, const int32_t* d_block_tables, int32_t max_blocks, float scale, int32_t window,

@@ -71,6 +71,7 @@ struct AttendPlan {
 };
 constexpr int kPairedRows = 8;             // half of a block
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv);
+int64_t attend_workspace_bound(int n_q, int n_kv, int head_dim, int total_q, int max_kv);
 bool attend_head_dim(int head_dim);
 int attend_rows_blocks(int head_dim);      // row blocks of a workgroup of launch_attend_rows, which takes heads of 64 and 128
 inline dim3 attend_grid(const AttendArgs& a) {      // places over two dimensions of less than 65536

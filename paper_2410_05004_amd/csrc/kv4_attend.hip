@@ -419,13 +419,21 @@ static int row_blocks(int head_dim, int64_t blocks, int64_t keys, int64_t tiles,
 // keys: 13.8 us in 128 workgroups, 12.1 in 256, 12.8 in 512), beyond that, where contexts are uneven and the last ones
 // would run alone, of 2048 (64 contexts of up to 8192 keys: 109 us in 512 workgroups, 89 in 2048; of up to 4000: 41 and 44), but not
 // for contexts of several workgroups, whose results are more to join (64 queries, 32000 keys: 59 us in 960 workgroups, 53 in 512).
+constexpr int kWholeKeys = 1280;
+struct ShareRule {
+  int workgroups, keys;                      // up to so many in all, of so many keys at least
+  bool one_tile;                             // only where contexts are a workgroup's
+};
+constexpr ShareRule kShareRules[] = {{kChipCUs, 128, false}, {2 * kChipCUs, 512, false}, {8 * kChipCUs, 2048, true}};
 static int key_shares(int64_t base, int64_t keys, bool one_tile) {
-  if (base <= 0 || keys <= 1280) return 1;
-  int64_t n = std::min<int64_t>(kChipCUs / base, keys / 128);
-  n = std::max(n, std::min<int64_t>(2 * kChipCUs / base, keys / 512));
-  if (one_tile) n = std::max(n, std::min<int64_t>(8 * kChipCUs / base, keys / 2048));
-  return (int)std::max<int64_t>(n, 1);
+  if (base <= 0 || keys <= kWholeKeys) return 1;
+  int64_t n = 1;
+  for (const ShareRule& r : kShareRules)
+    if (one_tile || !r.one_tile) n = std::max(n, std::min(r.workgroups / base, keys / r.keys));
+  return (int)n;
 }
+
+static int64_t row_bytes(int head_dim) { return 4 * (head_dim + 2); }       // of a row's share: see AttendArgs::part
 
 AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, int max_q, int max_kv) {
   AttendPlan p;
@@ -447,8 +455,23 @@ AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, 
   p.flat = rows > size;
   p.n_slots = (int)(p.flat ? all_rows / size + n_seq : n_seq);
   p.n_split = key_shares(tiles_of(size), max_kv, !p.flat && p.row_blocks <= 2);
-  p.workspace = p.n_split > 1 ? (int64_t)p.n_split * total_q * n_q * (head_dim + 2) * 4 : 0;
+  p.workspace = p.n_split > 1 ? p.n_split * ((int64_t)total_q * n_q) * row_bytes(head_dim) : 0;
   return p;
+}
+
+// Of calls of up to these sizes.  By a rule there are n <= workgroups / base shares, and base is at least n_kv, and at least rows / size
+// where workgroups have `size` rows: n * rows is at most workgroups / n_kv * rows, keys / r.keys * rows, and workgroups * size.  Each of
+// them, and with them the result, grows with the sizes or stays.
+int64_t attend_workspace_bound(int n_q, int n_kv, int head_dim, int total_q, int max_kv) {
+  if (max_kv <= kWholeKeys) return 0;
+  const int64_t rows = (int64_t)total_q * n_q;
+  const int few = head_dim == 256 ? 16 : 32, many = head_dim == 256 ? 16 : 16 * attend_rows_blocks(head_dim);     // see row_blocks
+  int64_t most = 0;
+  for (const ShareRule& r : kShareRules) {
+    const int64_t n = std::min(r.workgroups / n_kv, max_kv / r.keys);
+    if (n > 1) most = std::max(most, std::min(n * rows, (int64_t)r.workgroups * (r.one_tile ? few : many)));
+  }
+  return most * row_bytes(head_dim);
 }
 
 template <int HD>

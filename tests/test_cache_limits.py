@@ -1,5 +1,6 @@
 """Sizes at the limits of the entry points of the 4-bit cache and of pages as a whole, without a GPU."""
 import os
+import random
 import shutil
 import subprocess
 
@@ -23,3 +24,31 @@ def test_limits_on_the_host(tmp_path):
     assert r.returncode == 0, r.stderr[-3000:]
     run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert run.returncode == 0 and "limits ok" in run.stdout, run.stdout + run.stderr
+
+
+@pytest.mark.parametrize("n_q,n_kv,hd", [(32, 8, 128), (64, 8, 128), (40, 40, 128), (14, 2, 64), (4, 4, 64), (34, 1, 64), (16, 8, 256), (600, 600, 64)])
+def test_one_workspace_for_all_batches(n_q, n_kv, hd):
+    """A workspace of the bound of the largest batch serves every smaller one, although these may need more than the largest itself."""
+    import paper_2410_05004_amd as hc
+    desc = hc.ModelDesc(1, 256, n_q, n_kv, hd, 16, 4096, 2, 1e4, 1e-5, 0)
+    rng = random.Random(n_q + hd)
+
+    def size(hi):
+        return rng.choice([hi, rng.randint(0, hi), int(hi ** rng.random())])
+    for _ in range(60):
+        most_q, most_kv = size(2 ** 31 // n_q // 64), size(2 ** 20)
+        bound = hc.attend_kv4_workspace_bound(desc, most_q, most_kv)
+        assert bound <= 36 << 20
+        assert hc.attend_kv4_workspace_bound(desc, size(most_q), size(most_kv)) <= bound
+        for _ in range(60):
+            total_q = size(most_q)
+            n_seq, max_q = size(min(65535, max(total_q, 1))), size(max(total_q, 1))
+            assert hc.attend_kv4_workspace(desc, n_seq, total_q, max_q, size(most_kv)) <= bound
+    if (n_q, n_kv) == (32, 8):
+        assert hc.attend_kv4_workspace(desc, 64, 64, 1, 8192) > hc.attend_kv4_workspace(desc, 256, 256, 1, 8192)
+        assert hc.attend_kv4_workspace_bound(desc, 256, 8192) >= hc.attend_kv4_workspace(desc, 64, 64, 1, 8192)
+    assert hc.attend_kv4_workspace_bound(desc, 0, 1 << 20) == hc.attend_kv4_workspace_bound(desc, 1 << 10, 0) == 0
+    for args in ((-1, 1), (1, -1)):
+        with pytest.raises(hc.HCacheError) as e:
+            hc.attend_kv4_workspace_bound(desc, *args)
+        assert e.value.status == hc.HC_EINVAL
