@@ -350,7 +350,7 @@ hc_status hc_dequantize_kv(hc_ctx* ctx, int32_t layer, void* d_rows, const int32
  *   d_cu_q         int32 [n_seq + 1]     context s owns queries cu[s] .. cu[s + 1] - 1, cu[0] = 0
  *   d_kv_lens      int32 [n_seq]         keys of the context (those of this step's queries included, when they are stored)
  *   d_block_tables int32 [n_seq][max_blocks]
- *   scale          > 0: weights are softmax(scale * q . k)
+ *   scale          > 0: weights are softmax(scale * q . k); scale * log2(e), and with it every scaled score, within fp32's range
  *   d_out          bf16  [h_total_q][n_q_heads][head_dim], out_stride elements from one token to the next
  *   d_lse          fp32  [h_total_q][n_q_heads], or NULL: log of the sum of exp(scale * q . k) (natural), for joining with attention over
  *                        other keys
@@ -363,6 +363,7 @@ hc_status hc_dequantize_kv(hc_ctx* ctx, int32_t layer, void* d_rows, const int32
  * matrix instructions as two numbers of bf16, 2^-17 of it off at most, where contexts have up to 8 rows (h_max_q * n_q_heads /
  * n_kv_heads <= 8, and the context's queries too: single tokens mostly), so that outputs are rounded once; in all other calls as one, 2^-8 off at
  * most, each by itself (relative to their norm outputs are then off by some 0.0023, once rounded ones by 0.0017).  d_lse has the fp32 sums.
+ * Sums of weights, up to 2^8 each, times values are fp32 too: values within that factor of fp32's range overflow.
  *   d_workspace    16-byte aligned, workspace_bytes >= hc_attend_kv4_workspace of the same sizes (HC_EINVAL); used by this launch
  *                  alone until it is done: calls that may run at the same time, and graphs that may, need one each.  NULL when the
  *                  size is 0.

@@ -313,7 +313,8 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
   const hc_model_desc& d = ctx->desc;
   if (h_total_q < 0 || n_seq < 0 || h_max_q < 0 || h_max_kv < 0 || max_blocks < 0 || window < 0 || workspace_bytes < 0)
     return fail(HC_EINVAL, "negative size");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(HC_EINVAL, "scale must be positive and finite");
+  const float scale_log2 = scale * 1.44269504089f;
+  if (!(scale > 0.f) || !std::isfinite(scale_log2)) return fail(HC_EINVAL, "scale must be positive, and finite times log2(e)");
   if (h_total_q == 0 || n_seq == 0) return HC_OK;
   if (!d_q || !d_positions || !d_cu_q || !d_kv_lens || !d_block_tables || !d_out) return fail(HC_EINVAL, "null device pointer");
   const int64_t width = (int64_t)d.n_q_heads * d.head_dim;
@@ -357,7 +358,7 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
   a.n_kv = d.n_kv_heads;
   a.group = d.n_q_heads / d.n_kv_heads;
   a.window = window;
-  a.scale_log2 = scale * 1.44269504089f;
+  a.scale_log2 = scale_log2;
   a.flat = plan.flat;
   a.n_slots = plan.n_slots;
   a.n_split = plan.n_split;

@@ -38,8 +38,19 @@ static void large_pages() {
   }
 }
 
+// The kernels take scale * log2(e), which has to be finite too.
+static void large_scale() {
+  int32_t* i = reinterpret_cast<int32_t*>(mem);
+  hc_ctx c;
+  set(c, 1, 8, 2, 128, 16);
+  RETURNS(HC_OK, hc_set_kv4_pool(&c, 0, mem, 4));
+  for (float scale : {2.36e38f, 3.0e38f, 3.4028234e38f})
+    RETURNS(HC_EINVAL, hc_attend_kv4(&c, 0, mem, 1024, i, 1, i, i, 1, 1, 16, i, 1, scale, 0, mem, 1024, nullptr, nullptr, 0, nullptr));
+}
+
 int main() {
   large_pages();
+  large_scale();
   if (failures) return 1;
   std::printf("limits ok\n");
   return 0;
