@@ -531,6 +531,12 @@ hc_status hc_diag_route(int32_t d_model, int32_t d_kv, int32_t n_tok, int32_t n_
 hc_status hc_diag_tile(int32_t d_model, int32_t d_kv, int32_t n_tok, int32_t n_layers, int32_t norm_kind,
                        int32_t mode, int32_t* out_tile);
 
+/* Host-side view of an attention call of these sizes (no device work; hc_attend_kv4): out_plan[4] = { rows of a workgroup (queries x
+ * query heads of a KV head); 1 if there is a place for every tile of rows, 0 if for every context; shares of the keys; 1 if weights enter
+ * as two numbers of bf16 }. */
+hc_status hc_diag_attend_kv4(const hc_model_desc* desc, int32_t n_seq, int32_t h_total_q, int32_t h_max_q,
+                             int32_t h_max_kv, int32_t window, int32_t* out_plan);
+
 /* ---- measurement hooks -------------------------------------------------------------
  * Average duration in milliseconds of the restoration kernel launches (one per layer, or
  * one per group of layers under hc_restore_kv_layers) queued on

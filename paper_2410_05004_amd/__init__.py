@@ -24,6 +24,7 @@ from .binding import (  # noqa: F401
     kv4_page_bytes,
     attend_kv4_workspace,
     attend_kv4_workspace_bound,
+    diag_attend_kv4,
     HC_OK, HC_EINVAL, HC_ERANGE, HC_EALIGN, HC_ENOMEM, HC_EHIP, HC_ESTATE,
     HC_DEV_BAD_POSITION, HC_DEV_BAD_PAGE, HC_NORM_RMS, HC_NORM_LAYER,
     HC_POOL_KV, HC_POOL_KV4,

@@ -85,6 +85,7 @@ def _load():
                                 vp, i64, vp, vp, i64, vp]),
         "hc_attend_kv4_workspace": (i32, [p(ModelDesc), i32, i32, i32, i32, p(i64)]),
         "hc_attend_kv4_workspace_bound": (i32, [p(ModelDesc), i32, i32, p(i64)]),
+        "hc_diag_attend_kv4": (i32, [p(ModelDesc), i32, i32, i32, i32, i32, p(i32)]),
         "hc_fork_pages": (i32, [vp, i32, vp, i32, i32, vp, vp, vp, vp, i32, vp]),
         "hc_compact_pages": (i32, [vp, i32, vp, vp, i32, i32, vp, vp]),
         "hc_restore_contexts": (i32, [vp, vp, i32, vp, vp, vp, i32, vp, vp]),
@@ -124,7 +125,7 @@ EXPORTED = ("hc_last_error hc_version hc_validate_desc hc_create hc_destroy hc_s
             "hc_saver_flush hc_partition_layers hc_gather_kv hc_scatter_kv "
             "hc_restore_context_mixed hc_set_layer_weights_affine hc_saver_save_layer_deferred "
             "hc_saver_fence hc_restore_kv_layers hc_restore_contexts hc_timing_end_stats "
-            "hc_restore_context_static hc_static_stage_bytes hc_poison_staging hc_diag_mfma_duty hc_diag_tile_map hc_set_split hc_diag_split_plan hc_diag_route hc_diag_tile "
+            "hc_restore_context_static hc_static_stage_bytes hc_poison_staging hc_diag_mfma_duty hc_diag_tile_map hc_set_split hc_diag_split_plan hc_diag_route hc_diag_tile hc_diag_attend_kv4 "
             "hc_kv4_page_bytes hc_set_kv4_pool hc_quantize_kv hc_quantize_kv_pages hc_dequantize_kv hc_attend_kv4 "
             "hc_attend_kv4_workspace hc_attend_kv4_workspace_bound hc_fork_pages hc_compact_pages").split()
 
@@ -160,6 +161,13 @@ def diag_tile(d_model, d_kv, n_tok, n_layers=0, norm_kind=HC_NORM_RMS, mode=1):
     sums are worked out ahead of it."""
     out = (C.c_int32 * 4)()
     _check(lib.hc_diag_tile(d_model, d_kv, n_tok, n_layers, norm_kind, mode, out))
+    return tuple(out)
+
+
+def diag_attend_kv4(desc, n_seq, total_q, max_q, max_kv, window=0):
+    """hc_diag_attend_kv4: (rows of a workgroup, 1 if there is a place for every tile, shares of the keys, 1 if weights are in two parts)."""
+    out = (C.c_int32 * 4)()
+    _check(lib.hc_diag_attend_kv4(C.byref(desc), n_seq, total_q, max_q, max_kv, window, out))
     return tuple(out)
 
 

@@ -50,6 +50,14 @@ hc_status check_layer4(const hc_ctx* ctx, int32_t layer) {
   return HC_OK;
 }
 
+// A window leaves fewer keys to share than the sizes say; the workspace is that of all keys.
+AttendPlan plan_window(const hc_model_desc& d, const AttendPlan& all, int n_seq, int total_q, int max_q, int max_kv, int window) {
+  if (window == 0) return all;
+  AttendPlan plan = plan_attend(d.n_q_heads, d.n_kv_heads, d.head_dim, n_seq, total_q, max_q, (int)std::min<int64_t>(max_kv, (int64_t)window + max_q));
+  plan.n_split = std::min(plan.n_split, all.n_split);
+  return plan;
+}
+
 Kv4RowsArgs rows_args(const hc_ctx* ctx, int32_t layer, const int32_t* d_positions, int32_t n_tok, const int32_t* d_cu,
                       int32_t n_seq, const int32_t* d_tables, int32_t max_blocks) {
   const hc_layer_state& L = ctx->layers[layer];
@@ -302,6 +310,23 @@ hc_status hc_attend_kv4_workspace_bound(const hc_model_desc* desc, int32_t h_tot
   return HC_OK;
 }
 
+hc_status hc_diag_attend_kv4(const hc_model_desc* desc, int32_t n_seq, int32_t h_total_q, int32_t h_max_q, int32_t h_max_kv,
+                             int32_t window, int32_t* out_plan) {
+  clear_error();
+  if (!out_plan) return fail(HC_EINVAL, "null output pointer");
+  hc_status s = check_desc(desc);
+  if (s == HC_OK) s = check_kv4(*desc);
+  if (s != HC_OK) return s;
+  if (n_seq < 0 || h_total_q < 0 || h_max_q < 0 || h_max_kv < 0 || window < 0) return fail(HC_EINVAL, "negative size");
+  const AttendPlan all = plan_attend(desc->n_q_heads, desc->n_kv_heads, desc->head_dim, n_seq, h_total_q, h_max_q, h_max_kv);
+  const AttendPlan plan = plan_window(*desc, all, n_seq, h_total_q, h_max_q, h_max_kv, window);
+  out_plan[0] = 16 * plan.row_blocks;
+  out_plan[1] = plan.flat;
+  out_plan[2] = plan.n_split;
+  out_plan[3] = plan.paired;
+  return HC_OK;
+}
+
 hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_stride, const int32_t* d_positions,
                         int32_t h_total_q, const int32_t* d_cu_q, const int32_t* d_kv_lens, int32_t n_seq, int32_t h_max_q,
                         int32_t h_max_kv, const int32_t* d_block_tables, int32_t max_blocks, float scale, int32_t window,
@@ -328,11 +353,7 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
     if (!d_workspace || workspace_bytes < plan.workspace) return fail(HC_EINVAL, "workspace smaller than hc_attend_kv4_workspace says");
     if (!aligned16(d_workspace)) return fail(HC_EALIGN, "workspace not 16-byte aligned");
   }
-  if (window > 0) {       // a window leaves fewer keys to share than the sizes say; the workspace is that of all keys
-    const int n_split = plan.n_split;
-    plan = plan_attend(d.n_q_heads, d.n_kv_heads, d.head_dim, n_seq, h_total_q, h_max_q, (int)std::min<int64_t>(h_max_kv, (int64_t)window + h_max_q));
-    plan.n_split = std::min(plan.n_split, n_split);
-  }
+  plan = plan_window(d, plan, n_seq, h_total_q, h_max_q, h_max_kv, window);
   OnDevice on(ctx);
   HC_HIP(on.err);
   const hc_layer_state& L = ctx->layers[layer];
