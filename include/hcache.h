@@ -304,7 +304,9 @@ hc_status hc_restore_context_mixed(hc_ctx* ctx, const hc_store* hidden_store,
  * A layer may have, beside its bf16 pool or in its place, a pool of pages in 4 bits: 17 / 64 of the bytes.  32
  * neighbouring channels of a token's K or V row share a scale, the smallest power of two s with max|x| <= 7 s (2^-125 to
  * 2^125), and every value is stored as the nearest of +-s * {0, 0.5, 1, 1.5, 2, 3, 4, 6}, ties to the even code: at most
- * half a step from it.  What is read back is exact in bf16.  A group that holds an infinity or a NaN becomes NaN.
+ * half a step from it.  The scale's ends are two exceptions: where the largest passes 7 * 2^125 there is no larger scale, and values
+ * beyond 5 * 2^125 become 6 * 2^125; where it is 3.5 * 2^-125 or less the scale stays 2^-125, twice or more what it had to be.
+ * What is read back is exact in bf16.  A group that holds an infinity or a NaN becomes NaN.
  *   pool: uint8 [num_pages][n_kv_heads][block_size / 16][17 * head_dim]; the bytes of 16 tokens of a head are
  *     K codes  8 * head_dim  [token][channel / 2]                                  (even channel: low four bits)
  *     V codes  8 * head_dim  [token / 4][slice of 16][token % 4][head_dim / 32]    (slice r: channels r * head_dim / 16 ..)

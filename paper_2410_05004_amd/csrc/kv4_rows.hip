@@ -26,7 +26,7 @@ __device__ __forceinline__ int context_of(const int32_t* cu, int n_seq, int t, i
 // A workgroup takes 16 rows; 16 lanes take 128 columns of a row, 8 values (16 bytes) a lane, and go on in steps of
 // 128 * gridDim.y columns.  32 channels are four lanes: their largest magnitude is a maximum of bf16 patterns.
 //   scale = smallest 2^e with top <= 7 * 2^e: with top = 1.m * 2^E, e = E - 2 if 1.m <= 1.75, else E - 1
-// (then no value is further from its code than half a step); codes by the conversion instruction, to nearest, ties to even.
+// (then no value is further from its code than half a step, up to 7 * 2^125, where the scale ends: beyond, 6 * 2^125 is the nearest); codes by the conversion instruction, to nearest, ties to even.
 // Consecutive tokens make whole sub-blocks, so a workgroup's stores fill the lines that they touch.
 // Rows go past the caches, codes do not: they are what is read next, and fill lines by the store of several waves.
 // Bound: memory (2 + 17 / 32 bytes a value): 32768 tokens of 8 heads of 128, 170 MB, 38 us in, 31 out (4.5 and 5.5 TB/s; a large copy: 4.9; rows

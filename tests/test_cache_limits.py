@@ -4,7 +4,11 @@ import random
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
+
+import oracle.kv4_oracle as kv4
+import synthetic as syn
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -52,3 +56,22 @@ def test_one_workspace_for_all_batches(n_q, n_kv, hd):
         with pytest.raises(hc.HCacheError) as e:
             hc.attend_kv4_workspace_bound(desc, *args)
         assert e.value.status == hc.HC_EINVAL
+
+
+def test_where_the_scale_ends():
+    """Every finite bf16 value as a group's largest: at most half a step from its code up to 7 * 2^125, 6 * 2^125 beyond; the smallest
+    scale that reaches it, or 2^-125."""
+    bits = np.arange(1, 0x7F80, dtype=np.uint16)
+    top = syn.bf16_bits_to_f64(bits)
+    x = np.zeros((len(top), 32))
+    x[:, 0], x[:, 1] = top, -0.7 * top
+    code, scale = kv4.quantize(x)
+    got, s = kv4.dequantize(code, scale), 2.0 ** (scale[:, 0].astype(np.float64) - 127)
+    ends = top > 7 * 2.0 ** 125
+    assert 10 < ends.sum() < 128
+    assert np.all(got[ends, 0] == 6 * 2.0 ** 125) and np.all(s[ends] == 2.0 ** 125)
+    for c in (0, 1):
+        y, far = np.abs(x[~ends, c]) / s[~ends], np.abs(got[~ends, c] - x[~ends, c]) / s[~ends]
+        step = np.select([y < 2, y < 4], [0.5, 1], 2)
+        assert np.all(far <= step / 2)
+    assert np.all((top <= 7 * s) | ends) and np.all((top > 3.5 * s) | (s == 2.0 ** -125))
