@@ -7,8 +7,8 @@ namespace hc {
 // A workgroup takes 128 * NB rows, 32 * NB to a wave, and a share of the keys in tiles of 64.  Each wave decodes a quarter of
 // a tile into LDS, as the operands of v_mfma_f32_32x32x16 (1 KiB a fragment, 16 bytes a lane in lane order), while all of
 // them work on the tile before; the bytes of the tile behind are on their way to registers meanwhile.
-// Bound: issue: 8 contexts of up to 2048 queries on 4096 keys, 40 heads of 128, 454 GFLOP, 502 to 525 us (0.86 to 0.90 PFLOP/s; a large product of
-// the library's reaches 1.21), matrix instructions 43 % of the cycles and vector ones 49: of a wave's 32 rows and 64 keys, 32 matrix
+// Bound: issue: 8 contexts of up to 2048 queries on 4096 keys, 40 heads of 128, 454 GFLOP, 502 to 550 us (0.83 to 0.90 PFLOP/s, by
+// card; a large product of the library's reaches 1.21), matrix instructions 45 % of the cycles and vector ones 52: of a wave's 32 rows and 64 keys, 32 matrix
 // instructions of 32 cycles, the softmax's 2048 exponentials and its maxima and sums beside them, and a quarter of the tile's decoding.
 // Weights are rounded to bf16, 2^-8 relative at most (outputs are off by 0.0023 in norm, of which their own rounding makes 0.0017); the rest of
 // them in a second product: 846 us, so 1072 with it (8 times 2048 queries, 40 heads, up to 4096 keys).
@@ -143,7 +143,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
       float most[NB];
     };
     // Operands of 32 keys, read together: the compiler by itself reads each into the registers of the one before, right before its
-    // use, and waits (8 contexts of up to 2048 queries on 4096 keys, 40 heads of 128: 884 us, so 902; one on 16000 keys 737 and 785).
+    // use, and waits (8 contexts of 2048 queries on up to 4096 keys, 40 heads of 128, 846 us, so 864; one of 501 on 8692, 32 heads over 8, 91.6 and
+    // 92.8).  At 64 channels 10 registers go to scratch for it, 1 without: as fast either way (4 heads, 64 contexts of 512 on up to 4000 177 and 178).
     struct KeyParts {
       bf16x8 k[kSteps];
     };
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
   if (bad_page && lane == 0) atomicOr(a.err, HC_DEV_BAD_PAGE);
 }
 
-// blocks of 32 rows of a wave: as many as leave room for two waves in a SIMD's registers
+// blocks of 32 rows of a wave: as many as leave room for two waves in a SIMD's registers, all but a few at 64 channels
 constexpr int wave_blocks(int head_dim) { return head_dim == 64 ? 2 : 1; }
 
 int attend_rows_blocks(int head_dim) { return 8 * wave_blocks(head_dim); }
