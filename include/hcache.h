@@ -369,7 +369,8 @@ hc_status hc_dequantize_kv(hc_ctx* ctx, int32_t layer, void* d_rows, const int32
  *   d_workspace    16-byte aligned, workspace_bytes >= hc_attend_kv4_workspace of the same sizes (HC_EINVAL); used by this launch
  *                  alone until it is done: calls that may run at the same time, and graphs that may, need one each.  NULL when the
  *                  size is 0.
- * q_stride and out_stride: multiples of 8, at least n_q_heads * head_dim.  At most 65535 contexts (HC_ERANGE). */
+ * q_stride and out_stride: multiples of 8, at least n_q_heads * head_dim.  At most 65535 contexts, and h_total_q * n_q_heads below 2^31
+ * (HC_ERANGE, of the workspace too). */
 hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_stride, const int32_t* d_positions,
                         int32_t h_total_q, const int32_t* d_cu_q, const int32_t* d_kv_lens, int32_t n_seq, int32_t h_max_q,
                         int32_t h_max_kv, const int32_t* d_block_tables, int32_t max_blocks, float scale, int32_t window,

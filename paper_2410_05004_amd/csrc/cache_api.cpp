@@ -50,6 +50,13 @@ hc_status check_layer4(const hc_ctx* ctx, int32_t layer) {
   return HC_OK;
 }
 
+// What launches, and the plan's 64-bit products, have room for.
+hc_status check_attend_range(const hc_model_desc& d, int n_seq, int total_q) {
+  if (n_seq > 65535) return fail(HC_ERANGE, "at most 65535 contexts");
+  if ((int64_t)total_q * d.n_q_heads > INT_MAX) return fail(HC_ERANGE, "total_q * n_q_heads must stay below 2^31");
+  return HC_OK;
+}
+
 // A window leaves fewer keys to share than the sizes say; the workspace is that of all keys.
 AttendPlan plan_window(const hc_model_desc& d, const AttendPlan& all, int n_seq, int total_q, int max_q, int max_kv, int window) {
   if (window == 0) return all;
@@ -295,6 +302,8 @@ hc_status hc_attend_kv4_workspace(const hc_model_desc* desc, int32_t n_seq, int3
   if (s == HC_OK) s = check_kv4(*desc);
   if (s != HC_OK) return s;
   if (n_seq < 0 || h_total_q < 0 || h_max_q < 0 || h_max_kv < 0) return fail(HC_EINVAL, "negative size");
+  s = check_attend_range(*desc, n_seq, h_total_q);
+  if (s != HC_OK) return s;
   *out_bytes = plan_attend(desc->n_q_heads, desc->n_kv_heads, desc->head_dim, n_seq, h_total_q, h_max_q, h_max_kv).workspace;
   return HC_OK;
 }
@@ -318,6 +327,8 @@ hc_status hc_diag_attend_kv4(const hc_model_desc* desc, int32_t n_seq, int32_t h
   if (s == HC_OK) s = check_kv4(*desc);
   if (s != HC_OK) return s;
   if (n_seq < 0 || h_total_q < 0 || h_max_q < 0 || h_max_kv < 0 || window < 0) return fail(HC_EINVAL, "negative size");
+  s = check_attend_range(*desc, n_seq, h_total_q);
+  if (s != HC_OK) return s;
   const AttendPlan all = plan_attend(desc->n_q_heads, desc->n_kv_heads, desc->head_dim, n_seq, h_total_q, h_max_q, h_max_kv);
   const AttendPlan plan = plan_window(*desc, all, n_seq, h_total_q, h_max_q, h_max_kv, window);
   out_plan[0] = 16 * plan.row_blocks;
@@ -346,8 +357,8 @@ hc_status hc_attend_kv4(hc_ctx* ctx, int32_t layer, const void* d_q, int64_t q_s
   if (q_stride < width || q_stride % 8 || out_stride < width || out_stride % 8)
     return fail(HC_EINVAL, "strides must be multiples of 8 of at least n_q_heads * head_dim");
   if (!aligned16(d_q) || !aligned16(d_out)) return fail(HC_EALIGN, "queries or output not 16-byte aligned");
-  if (n_seq > 65535) return fail(HC_ERANGE, "at most 65535 contexts");
-  if ((int64_t)h_total_q * d.n_q_heads > INT_MAX) return fail(HC_ERANGE, "total_q * n_q_heads must stay below 2^31");
+  s = check_attend_range(d, n_seq, h_total_q);
+  if (s != HC_OK) return s;
   AttendPlan plan = plan_attend(d.n_q_heads, d.n_kv_heads, d.head_dim, n_seq, h_total_q, h_max_q, h_max_kv);
   if (plan.workspace) {
     if (!d_workspace || workspace_bytes < plan.workspace) return fail(HC_EINVAL, "workspace smaller than hc_attend_kv4_workspace says");

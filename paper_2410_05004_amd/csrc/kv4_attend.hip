@@ -14,6 +14,7 @@
 // Decoded keys and values are exact in bf16; W is rounded to bf16 (2^-8 relative at most, without a bias, which averages out over
 // the keys), in two parts where rows are few (see PAIRED); sums and statistics are fp32.
 #include <algorithm>
+#include <climits>
 
 #include "kv4_device.h"
 
@@ -464,7 +465,7 @@ AttendPlan plan_attend(int n_q, int n_kv, int head_dim, int n_seq, int total_q, 
 // them, and with them the result, grows with the sizes or stays.
 int64_t attend_workspace_bound(int n_q, int n_kv, int head_dim, int total_q, int max_kv) {
   if (max_kv <= kWholeKeys) return 0;
-  const int64_t rows = (int64_t)total_q * n_q;
+  const int64_t rows = std::min<int64_t>((int64_t)total_q * n_q, INT_MAX);      // calls have no more
   const int few = head_dim == 256 ? 16 : 32, many = head_dim == 256 ? 16 : 16 * attend_rows_blocks(head_dim);     // see row_blocks
   int64_t most = 0;
   for (const ShareRule& r : kShareRules) {

@@ -48,8 +48,28 @@ static void large_scale() {
     RETURNS(HC_EINVAL, hc_attend_kv4(&c, 0, mem, 1024, i, 1, i, i, 1, 1, 16, i, 1, scale, 0, mem, 1024, nullptr, nullptr, 0, nullptr));
 }
 
+// More rows than a call may have: its workspace and layout are refused as the call is, and the bound is that of the most there may be.
+static void many_rows() {
+  struct { int n_q, n_kv, total_q; } sizes[] = {{1 << 20, 8, 2048}, {64, 8, INT32_MAX}, {1 << 30, 1 << 14, INT32_MAX}, {INT32_MAX, 1, INT32_MAX}};
+  for (auto& z : sizes) {
+    hc_ctx c;
+    set(c, 1, z.n_q, z.n_kv, 64, 16);
+    int64_t bytes = -1;
+    int32_t plan[4];
+    RETURNS(HC_ERANGE, hc_attend_kv4_workspace(&c.desc, 1, z.total_q, z.total_q, INT32_MAX, &bytes));
+    RETURNS(HC_ERANGE, hc_diag_attend_kv4(&c.desc, 1, z.total_q, z.total_q, INT32_MAX, 7, plan));
+    RETURNS(HC_ERANGE, hc_attend_kv4_workspace(&c.desc, 65536, 1, 1, INT32_MAX, &bytes));
+    RETURNS(HC_OK, hc_attend_kv4_workspace_bound(&c.desc, z.total_q, INT32_MAX, &bytes));
+    if (bytes < 0 || bytes > 36 << 20) {
+      std::printf("bound of %lld bytes\n", (long long)bytes);
+      ++failures;
+    }
+  }
+}
+
 int main() {
   large_pages();
+  many_rows();
   large_scale();
   if (failures) return 1;
   std::printf("limits ok\n");
